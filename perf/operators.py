@@ -282,7 +282,7 @@ def _own(s):
         return dict(dx=s["dx"], dw=s["dw"])
     if case["op"] == "linear":
         if case["q8"]:
-            ctx.linear_q8(s["x"], s["x_scale"], T, n, s["W"], s["w_scale"], m, s["bias"], act, s["res"], s["pre"], s["y"])
+            ctx.linear_scaled(s["x"], s["x_scale"], T, n, s["W"], s["w_scale"], m, s["bias"], act, s["res"], s["pre"], s["y"])
         else:
             ctx.linear(s["x"], T, n, s["W"], m, s["bias"], act, s["res"], s["pre"], s["y"])
         return dict(y=s["y"], pre=s["pre"]) if case["pre"] else dict(y=s["y"])
