@@ -349,6 +349,39 @@ int unipool_stack_aux_loss(unipool_ctx* ctx, const unipool_stack* stack, int32_t
 int unipool_stack_backward(unipool_ctx* ctx, const unipool_stack* stack, int32_t T, int32_t flags,
                            unipool_stream stream);
 
+/* RMS norm of the residual stream with the addition in front of it (the pre-normalised block of the LLaMA-style
+ * backbone, App. B, App. D), for rows of any width from 1 to 16384:
+ *   r = x + y;  n_t = 1 / sqrt(mean_j r_tj^2 + eps);  h = r * n_t * w;
+ *   q = e4m3(h / s_t) with s_t = max(max_j |h_tj| / 448, 2^-126), rounded to nearest even.
+ * The statistics are fp32 and h is formed from the unrounded sum; each output is rounded once.  A row that holds
+ * a NaN has NaN in rstd, h, q and q_scale; infinities follow the formulas.
+ * in : x [T,width] (ctx dtype); y [T,width] or NULL (r = x); w [width] float; eps >= 0.
+ * out: r [T,width] (ctx dtype) or NULL; rstd [T] float (n_t, kept for the backward call) or NULL; h [T,width]
+ *      (ctx dtype) or NULL; q [T,width] e4m3 (one byte each) and q_scale [T] float, or both NULL; h or q is given.
+ *      r and h may each be x or y. */
+int unipool_rmsnorm(unipool_ctx* ctx, const void* x, const void* y, int32_t T, int32_t width, const float* w, float eps,
+                    void* r, float* rstd, void* h, uint8_t* q, float* q_scale, unipool_stream stream);
+
+/* Backward of unipool_rmsnorm.  With c_t = sum_j dh_tj w_j r_tj:
+ *   dx = rstd w dh - r rstd^3 c / width (+ dr),   dw_j += sum_t dh_tj rstd_t r_tj
+ * (dx is the gradient of x and of y alike; dr that of r itself, which the residual stream brings).
+ * in : dh [T,width]; r [T,width] as the forward call stored it (its x where it had no y); w; rstd; dr [T,width] or
+ *      NULL; scratch: unipool_rmsnorm_bwd_scratch() bytes of device memory, 16-byte aligned, which the call may
+ *      use until it is complete on the stream (NULL where dw is).
+ * out: dx [T,width] (ctx dtype, overwritten; may be dh, r or dr); dw [width] float +=, or NULL.
+ * flags: 0 or UNIPOOL_WGRAD_OVERWRITE (dw is written, not added to).  The sums over the rows are taken in an order
+ * that depends on T and width alone. */
+int unipool_rmsnorm_bwd(unipool_ctx* ctx, const void* dh, const void* r, int32_t T, int32_t width, const float* w,
+                        const float* rstd, const void* dr, void* dx, float* dw, void* scratch, int32_t flags,
+                        unipool_stream stream);
+size_t unipool_rmsnorm_bwd_scratch(const unipool_ctx* ctx, int32_t T, int32_t width);   /* host function */
+
+/* Rows in 8 bits with a scale each, as unipool_rmsnorm writes them: for the weights of unipool_linear_scaled (rows =
+ * output features) and for its input where that does not come from a norm.
+ * in : x [rows,width] (ctx dtype), rows of any number.  out: q [rows,width] e4m3; q_scale [rows] float. */
+int unipool_quantize_rows(unipool_ctx* ctx, const void* x, int32_t rows, int32_t width, uint8_t* q, float* q_scale,
+                          unipool_stream stream);
+
 /* Distinct-expert accounting (App. E): U(x) = |{ e_l(x) : l = 1..L }|, the number of different pool
  * experts a token selects over all layers (the paper states it for top-1; with top-k every selected
  * expert of every layer counts).  With the shared pool 1 <= U <= min(M, L k); with private experts
@@ -386,7 +419,8 @@ enum {
   UNIPOOL_PH_COMBINE, UNIPOOL_PH_POOL_AUX, UNIPOOL_PH_BWD_SCALE_GATHER, UNIPOOL_PH_BWD_DGATE,
   UNIPOOL_PH_DGRAD_DOWN, UNIPOOL_PH_DGRAD_GU, UNIPOOL_PH_WGRAD_DOWN, UNIPOOL_PH_WGRAD_GU,
   UNIPOOL_PH_UNPERMUTE_SUM, UNIPOOL_PH_ROUTE_BWD_DZ, UNIPOOL_PH_ROUTE_BWD_DX,
-  UNIPOOL_PH_ROUTE_BWD_DW, UNIPOOL_N_PHASES
+  UNIPOOL_PH_ROUTE_BWD_DW, UNIPOOL_PH_RMSNORM, UNIPOOL_PH_RMSNORM_BWD, UNIPOOL_PH_LINEAR, UNIPOOL_PH_LINEAR_BWD,
+  UNIPOOL_N_PHASES
 };
 int unipool_profile_enable(unipool_ctx* ctx, int32_t on);
 int unipool_profile_read(unipool_ctx* ctx, double* ms, int64_t* launches);

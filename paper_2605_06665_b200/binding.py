@@ -18,6 +18,7 @@ ROUTER_NORM, ROUTER_SOFTMAX = 0, 1
 ROW_ALIGN = 128
 BWD_SKIP_WGRAD = 1
 WGRAD_OVERWRITE = 2
+ACTIVATIONS = {"none": 0, "relu": 1, "silu": 2, "gelu": 3}
 STACK_NO_AUX = 4
 STACK_LEAVE_WGRAD = 8
 
@@ -30,12 +31,14 @@ EXPORTS = (
     "unipool_unique_experts", "unipool_router_prepare", "unipool_selftest_wait",
     "unipool_stack_forward", "unipool_stack_aux_loss", "unipool_stack_backward",
     "unipool_gemm_kernel", "unipool_dispatch_rows", "unipool_expert_fwd_rows", "unipool_expert_bwd_rows", "unipool_pool_wgrad_rows",
+    "unipool_rmsnorm", "unipool_rmsnorm_bwd", "unipool_rmsnorm_bwd_scratch", "unipool_quantize_rows",
 )
 
 PHASES = (
     "route_logits", "route_select", "dispatch_maps", "dispatch_gather", "expert_fwd_gu", "expert_fwd_down",
     "combine", "pool_aux", "bwd_scale_gather", "bwd_dgate", "dgrad_down", "dgrad_gu", "wgrad_down", "wgrad_gu",
     "unpermute_sum", "route_bwd_dz", "route_bwd_dx", "route_bwd_dw",
+    "rmsnorm", "rmsnorm_bwd", "linear", "linear_bwd",
 )
 
 
@@ -131,6 +134,14 @@ def lib():
     L.unipool_gemm_kernel.argtypes = [vp, i32, i32, i32]
     L.unipool_unique_experts.restype = ctypes.c_int
     L.unipool_unique_experts.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp]
+    L.unipool_rmsnorm.restype = ctypes.c_int
+    L.unipool_rmsnorm.argtypes = [vp, vp, vp, i32, i32, vp, f32, vp, vp, vp, vp, vp, vp]
+    L.unipool_rmsnorm_bwd.restype = ctypes.c_int
+    L.unipool_rmsnorm_bwd.argtypes = [vp, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp, i32, vp]
+    L.unipool_rmsnorm_bwd_scratch.restype = ctypes.c_size_t
+    L.unipool_rmsnorm_bwd_scratch.argtypes = [vp, i32, i32]
+    L.unipool_quantize_rows.restype = ctypes.c_int
+    L.unipool_quantize_rows.argtypes = [vp, vp, i32, i32, vp, vp, vp]
     L.unipool_calibrate_c.restype = ctypes.c_int
     L.unipool_calibrate_c.argtypes = [vp, i32, i32, i32, ctypes.c_uint64, ctypes.POINTER(f32), vp]
     L.unipool_selftest_wait.restype = ctypes.c_int
@@ -266,6 +277,26 @@ class Context:
 
     def stack_backward(self, stack, T, flags=0):
         _check(lib().unipool_stack_backward(self.handle, ctypes.byref(stack), T, flags, _stream()))
+
+    # ---- the operators around the MoE layer
+    def rmsnorm(self, x, y, T, width, w, eps, r, rstd, h, q=None, q_scale=None):
+        _check(lib().unipool_rmsnorm(self.handle, _p(x), _p(y), T, width, _p(w), eps, _p(r), _p(rstd), _p(h), _p(q),
+                                     _p(q_scale), _stream()))
+
+    def rmsnorm_bwd(self, dh, r, T, width, w, rstd, dr, dx, dw, flags=0, scratch=None):
+        """``scratch``: a device tensor of unipool_rmsnorm_bwd_scratch() bytes; allocated per call if None."""
+        if scratch is None and dw is not None:
+            scratch = self._scratch(lib().unipool_rmsnorm_bwd_scratch(self.handle, T, width))
+        _check(lib().unipool_rmsnorm_bwd(self.handle, _p(dh), _p(r), T, width, _p(w), _p(rstd), _p(dr), _p(dx), _p(dw),
+                                         _p(scratch), flags, _stream()))
+
+    def quantize_rows(self, x, rows, width, q, q_scale):
+        _check(lib().unipool_quantize_rows(self.handle, _p(x), rows, width, _p(q), _p(q_scale), _stream()))
+
+    def _scratch(self, nbytes):
+        """Device memory for one call: the allocator hands it on to later work of the same stream only."""
+        import torch
+        return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self.device)
 
     def unique_experts(self, idx, expert_base, L, T, unique, total):
         _check(lib().unipool_unique_experts(self.handle, _p(idx), _p(expert_base), L, T, _p(unique), _p(total),

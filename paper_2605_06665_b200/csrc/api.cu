@@ -115,6 +115,9 @@ using namespace unipool;
 
 #define CHECK_CTX(ctx) UP_REQUIRE((ctx) != nullptr, UNIPOOL_ERR_INVALID_ARG, "ctx is NULL")
 #define CHECK_PTR(p) UP_REQUIRE((p) != nullptr, UNIPOOL_ERR_INVALID_ARG, #p " is NULL")
+#define CHECK_SCRATCH(p)                                                             \
+  UP_REQUIRE((p) != nullptr && (reinterpret_cast<uintptr_t>(p) & 15) == 0,           \
+             UNIPOOL_ERR_WORKSPACE, #p " must be a 16-byte aligned device pointer")
 #define CHECK_T(ctx, T)                                                              \
   UP_REQUIRE((T) >= 0 && (T) <= (ctx)->cfg.max_tokens, UNIPOOL_ERR_INVALID_ARG,      \
              "T = %d outside [0, max_tokens = %d]", (int)(T), (ctx)->cfg.max_tokens)
@@ -403,6 +406,44 @@ int unipool_route_bwd(unipool_ctx* ctx, const void* x, int32_t T, const float* W
   CHECK_PTR(dgate); CHECK_PTR(dx); CHECK_PTR(dW_r); CHECK_PTR(dsigma);
   return route_bwd_launch(ctx, x, T, W_r, sigma, n_experts, znorm, z_saved, idx, dgate,
                           dscore_coef, dx, dW_r, dsigma, static_cast<cudaStream_t>(stream));
+}
+
+#define CHECK_WIDTH(n)                                                                           \
+  UP_REQUIRE((n) >= 1 && (n) <= norm_max_width(), UNIPOOL_ERR_UNSUPPORTED, "width = %d outside [1, %d]", (int)(n), \
+             norm_max_width())
+
+int unipool_rmsnorm(unipool_ctx* ctx, const void* x, const void* y, int32_t T, int32_t width, const float* w, float eps,
+                    void* r, float* rstd, void* h, uint8_t* q, float* q_scale, unipool_stream stream) {
+  CHECK_CTX(ctx); CHECK_T(ctx, T); CHECK_WIDTH(width);
+  CHECK_PTR(x); CHECK_PTR(w);
+  UP_REQUIRE(eps >= 0.f, UNIPOOL_ERR_INVALID_ARG, "eps must be >= 0");
+  UP_REQUIRE(h != nullptr || q != nullptr, UNIPOOL_ERR_INVALID_ARG, "h and q are both NULL");
+  UP_REQUIRE((q != nullptr) == (q_scale != nullptr), UNIPOOL_ERR_INVALID_ARG, "q and q_scale go together");
+  UP_REQUIRE(r == nullptr || r != h, UNIPOOL_ERR_INVALID_ARG, "r and h are the same array");
+  return rmsnorm_launch(ctx, x, y, T, width, w, eps, r, rstd, h, q, q_scale, static_cast<cudaStream_t>(stream));
+}
+
+size_t unipool_rmsnorm_bwd_scratch(const unipool_ctx* ctx, int32_t T, int32_t width) {
+  return ctx == nullptr || T < 1 || width < 1 ? 0 : rmsnorm_bwd_scratch(ctx, T, width);
+}
+
+int unipool_rmsnorm_bwd(unipool_ctx* ctx, const void* dh, const void* r, int32_t T, int32_t width, const float* w,
+                        const float* rstd, const void* dr, void* dx, float* dw, void* scratch, int32_t flags,
+                        unipool_stream stream) {
+  CHECK_CTX(ctx); CHECK_T(ctx, T); CHECK_WIDTH(width);
+  CHECK_PTR(dh); CHECK_PTR(r); CHECK_PTR(w); CHECK_PTR(rstd); CHECK_PTR(dx);
+  UP_REQUIRE((flags & ~UNIPOOL_WGRAD_OVERWRITE) == 0, UNIPOOL_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+  if (dw != nullptr && T > 0) CHECK_SCRATCH(scratch);
+  return rmsnorm_bwd_launch(ctx, dh, r, T, width, w, rstd, dr, dx, dw, static_cast<float*>(scratch),
+                            (flags & UNIPOOL_WGRAD_OVERWRITE) != 0, static_cast<cudaStream_t>(stream));
+}
+
+int unipool_quantize_rows(unipool_ctx* ctx, const void* x, int32_t rows, int32_t width, uint8_t* q, float* q_scale,
+                          unipool_stream stream) {
+  CHECK_CTX(ctx); CHECK_WIDTH(width);
+  UP_REQUIRE(rows >= 0, UNIPOOL_ERR_INVALID_ARG, "rows = %d is negative", rows);
+  CHECK_PTR(x); CHECK_PTR(q); CHECK_PTR(q_scale);
+  return quantize_rows_launch(ctx, x, rows, width, q, q_scale, static_cast<cudaStream_t>(stream));
 }
 
 int unipool_unique_experts(unipool_ctx* ctx, const int32_t* idx, const int32_t* expert_base, int32_t L,

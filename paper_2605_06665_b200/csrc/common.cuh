@@ -226,6 +226,14 @@ int guard_check_launch(unipool_ctx*, cudaStream_t);
 int calibrate_launch(unipool_ctx*, int n_experts, int top_k, int n_samples, uint64_t seed,
                      float* c_out, cudaStream_t);
 
+int norm_max_width();
+int rmsnorm_launch(unipool_ctx*, const void* x, const void* y, int T, int width, const float* w, float eps, void* r,
+                   float* rstd, void* h, uint8_t* q, float* q_scale, cudaStream_t);
+size_t rmsnorm_bwd_scratch(const unipool_ctx*, int T, int width);
+int rmsnorm_bwd_launch(unipool_ctx*, const void* dh, const void* r, int T, int width, const float* w, const float* rstd,
+                       const void* dr, void* dx, float* dw, float* scratch, bool overwrite, cudaStream_t);
+int quantize_rows_launch(unipool_ctx*, const void* x, int rows, int width, uint8_t* q, float* q_scale, cudaStream_t);
+
 // grouped GEMMs: CUDA-core path (fp32 mode) and tcgen05 path (bf16 mode)
 struct ExpertFwdArgs {
   const void* Xp; const int32_t* offsets; const int32_t* tile_expert;
