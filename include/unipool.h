@@ -382,6 +382,47 @@ size_t unipool_rmsnorm_bwd_scratch(const unipool_ctx* ctx, int32_t T, int32_t wi
 int unipool_quantize_rows(unipool_ctx* ctx, const void* x, int32_t rows, int32_t width, uint8_t* q, float* q_scale,
                           unipool_stream stream);
 
+/* activations of the dense products */
+#define UNIPOOL_ACT_NONE 0
+#define UNIPOOL_ACT_RELU 1
+#define UNIPOOL_ACT_SILU 2      /* p / (1 + exp(-p))                                              */
+#define UNIPOOL_ACT_GELU 3      /* 0.5 p (1 + tanh(sqrt(2/pi) (p + 0.044715 p^3)))                */
+
+/* Dense product with its epilogue, for the layers beside the experts (projections, dense FFN layers):
+ *   p = x W^T + bias,  y = act(p) + residual,
+ * accumulated in fp32, each output rounded once.  n_in and n_out are multiples of 64, independent of d_model and
+ * d_ff.
+ * in : x [T,n_in]; W [n_out,n_in] (ctx dtype); bias [n_out] float or NULL; act UNIPOOL_ACT_*; residual [T,n_out]
+ *      (ctx dtype) or NULL.
+ * out: y [T,n_out] (ctx dtype; may be residual); pre [T,n_out] (ctx dtype; p, which the backward call of an
+ *      activation needs) or NULL.
+ * In a bf16 context the arrays of ctx dtype are 16-byte aligned. */
+int unipool_linear(unipool_ctx* ctx, const void* x, int32_t T, int32_t n_in, const void* W, int32_t n_out,
+                   const float* bias, int32_t act, const void* residual, void* pre, void* y, unipool_stream stream);
+
+/* The same of operands in e4m3 with a scale for each token and each output feature (unipool_rmsnorm,
+ * unipool_quantize_rows), in a bf16 context: p = x_scale[t] w_scale[o] sum_i x_ti W_oi + bias_o.  Both operands are
+ * 16-byte aligned. */
+int unipool_linear_scaled(unipool_ctx* ctx, const uint8_t* x, const float* x_scale, int32_t T, int32_t n_in,
+                          const uint8_t* W, const float* w_scale, int32_t n_out, const float* bias, int32_t act,
+                          const void* residual, void* pre, void* y, unipool_stream stream);
+
+/* Backward of unipool_linear:
+ *   dp = dy act'(p);  dx = dp W (+ dx_residual);  dW += dp^T x;  dbias += sum_t dp
+ * (the residual's gradient is dy).  dp is rounded to the ctx dtype, as an operand of both products; dbias sums the
+ * unrounded values.  Sums are taken in an order that depends on the sizes alone.
+ * in : dy [T,n_out]; pre [T,n_out] of the forward call and dp [T,n_out], scratch that is overwritten (both NULL
+ *      with UNIPOOL_ACT_NONE; dp may be pre or dy); x, W of the forward call (x is needed for dW, W for dx);
+ *      dx_residual [T,n_in] or NULL; scratch: unipool_linear_bwd_scratch() bytes of device memory, 16-byte aligned,
+ *      which the call may use until it is complete on the stream (NULL where dW and dbias are).
+ * out: dx [T,n_in] (ctx dtype, overwritten; may be dx_residual) or NULL; dW [n_out,n_in] float += or NULL (16-byte
+ *      aligned in a bf16 context); dbias [n_out] float += or NULL.
+ * flags: 0 or UNIPOOL_WGRAD_OVERWRITE (dW and dbias are written, not added to). */
+int unipool_linear_bwd(unipool_ctx* ctx, const void* dy, int32_t T, int32_t n_out, const void* pre, int32_t act,
+                       const void* x, int32_t n_in, const void* W, void* dp, const void* dx_residual, void* dx, float* dW,
+                       float* dbias, void* scratch, int32_t flags, unipool_stream stream);
+size_t unipool_linear_bwd_scratch(const unipool_ctx* ctx, int32_t T, int32_t n_in, int32_t n_out);   /* host function */
+
 /* Distinct-expert accounting (App. E): U(x) = |{ e_l(x) : l = 1..L }|, the number of different pool
  * experts a token selects over all layers (the paper states it for top-1; with top-k every selected
  * expert of every layer counts).  With the shared pool 1 <= U <= min(M, L k); with private experts

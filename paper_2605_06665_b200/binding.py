@@ -32,6 +32,7 @@ EXPORTS = (
     "unipool_stack_forward", "unipool_stack_aux_loss", "unipool_stack_backward",
     "unipool_gemm_kernel", "unipool_dispatch_rows", "unipool_expert_fwd_rows", "unipool_expert_bwd_rows", "unipool_pool_wgrad_rows",
     "unipool_rmsnorm", "unipool_rmsnorm_bwd", "unipool_rmsnorm_bwd_scratch", "unipool_quantize_rows",
+    "unipool_linear", "unipool_linear_scaled", "unipool_linear_bwd", "unipool_linear_bwd_scratch",
 )
 
 PHASES = (
@@ -142,6 +143,14 @@ def lib():
     L.unipool_rmsnorm_bwd_scratch.argtypes = [vp, i32, i32]
     L.unipool_quantize_rows.restype = ctypes.c_int
     L.unipool_quantize_rows.argtypes = [vp, vp, i32, i32, vp, vp, vp]
+    L.unipool_linear.restype = ctypes.c_int
+    L.unipool_linear.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp]
+    L.unipool_linear_scaled.restype = ctypes.c_int
+    L.unipool_linear_scaled.argtypes = [vp, vp, vp, i32, i32, vp, vp, i32, vp, i32, vp, vp, vp, vp]
+    L.unipool_linear_bwd.restype = ctypes.c_int
+    L.unipool_linear_bwd.argtypes = [vp, vp, i32, i32, vp, i32, vp, i32, vp, vp, vp, vp, vp, vp, vp, i32, vp]
+    L.unipool_linear_bwd_scratch.restype = ctypes.c_size_t
+    L.unipool_linear_bwd_scratch.argtypes = [vp, i32, i32, i32]
     L.unipool_calibrate_c.restype = ctypes.c_int
     L.unipool_calibrate_c.argtypes = [vp, i32, i32, i32, ctypes.c_uint64, ctypes.POINTER(f32), vp]
     L.unipool_selftest_wait.restype = ctypes.c_int
@@ -292,6 +301,22 @@ class Context:
 
     def quantize_rows(self, x, rows, width, q, q_scale):
         _check(lib().unipool_quantize_rows(self.handle, _p(x), rows, width, _p(q), _p(q_scale), _stream()))
+
+    def linear(self, x, T, n_in, W, n_out, bias, act, residual, pre, y):
+        """``act``: a value of ACTIVATIONS."""
+        _check(lib().unipool_linear(self.handle, _p(x), T, n_in, _p(W), n_out, _p(bias), act, _p(residual), _p(pre), _p(y),
+                                    _stream()))
+
+    def linear_scaled(self, x, x_scale, T, n_in, W, w_scale, n_out, bias, act, residual, pre, y):
+        _check(lib().unipool_linear_scaled(self.handle, _p(x), _p(x_scale), T, n_in, _p(W), _p(w_scale), n_out, _p(bias),
+                                           act, _p(residual), _p(pre), _p(y), _stream()))
+
+    def linear_bwd(self, dy, T, n_out, pre, act, x, n_in, W, dp, dx_residual, dx, dW, dbias, flags=0, scratch=None):
+        """``scratch``: a device tensor of unipool_linear_bwd_scratch() bytes; allocated per call if None."""
+        if scratch is None and (dW is not None or dbias is not None):
+            scratch = self._scratch(lib().unipool_linear_bwd_scratch(self.handle, T, n_in, n_out))
+        _check(lib().unipool_linear_bwd(self.handle, _p(dy), T, n_out, _p(pre), act, _p(x), n_in, _p(W), _p(dp),
+                                        _p(dx_residual), _p(dx), _p(dW), _p(dbias), _p(scratch), flags, _stream()))
 
     def _scratch(self, nbytes):
         """Device memory for one call: the allocator hands it on to later work of the same stream only."""

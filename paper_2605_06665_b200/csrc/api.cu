@@ -446,6 +446,63 @@ int unipool_quantize_rows(unipool_ctx* ctx, const void* x, int32_t rows, int32_t
   return quantize_rows_launch(ctx, x, rows, width, q, q_scale, static_cast<cudaStream_t>(stream));
 }
 
+#define CHECK_FEATURES(n)                                                                        \
+  UP_REQUIRE((n) >= 64 && (n) <= (1 << 24) && (n) % 64 == 0, UNIPOOL_ERR_UNSUPPORTED,            \
+             #n " = %d must be a multiple of 64 (2^24 at most)", (int)(n))
+#define CHECK_ACT(a)                                                                             \
+  UP_REQUIRE((a) >= UNIPOOL_ACT_NONE && (a) <= UNIPOOL_ACT_GELU, UNIPOOL_ERR_INVALID_ARG, "act = %d", (int)(a))
+// (the tensor-core path moves these by TMA)
+#define CHECK_ALIGNED(ctx, p)                                                                    \
+  UP_REQUIRE(!use_tensor_cores(ctx) || (reinterpret_cast<uintptr_t>(p) & 15) == 0, UNIPOOL_ERR_INVALID_ARG, \
+             #p " is not 16-byte aligned")
+
+static int linear_call(unipool_ctx* ctx, const LinearArgs& a, unipool_stream stream) {
+  const void *x = a.x, *W = a.W, *residual = a.residual, *pre = a.pre, *y = a.y;
+  const int n_in = a.n_in, n_out = a.n_out;
+  CHECK_T(ctx, a.T); CHECK_FEATURES(n_in); CHECK_FEATURES(n_out); CHECK_ACT(a.act);
+  CHECK_PTR(x); CHECK_PTR(W); CHECK_PTR(y);
+  UP_REQUIRE(pre == nullptr || (pre != y && pre != residual), UNIPOOL_ERR_INVALID_ARG, "pre is y or residual");
+  CHECK_ALIGNED(ctx, x); CHECK_ALIGNED(ctx, W); CHECK_ALIGNED(ctx, residual); CHECK_ALIGNED(ctx, pre); CHECK_ALIGNED(ctx, y);
+  return linear_launch(ctx, a, static_cast<cudaStream_t>(stream));
+}
+
+int unipool_linear(unipool_ctx* ctx, const void* x, int32_t T, int32_t n_in, const void* W, int32_t n_out,
+                   const float* bias, int32_t act, const void* residual, void* pre, void* y, unipool_stream stream) {
+  CHECK_CTX(ctx);
+  return linear_call(ctx, LinearArgs{x, W, nullptr, nullptr, T, n_in, n_out, act, bias, residual, pre, y}, stream);
+}
+
+int unipool_linear_scaled(unipool_ctx* ctx, const uint8_t* x, const float* x_scale, int32_t T, int32_t n_in,
+                          const uint8_t* W, const float* w_scale, int32_t n_out, const float* bias, int32_t act,
+                          const void* residual, void* pre, void* y, unipool_stream stream) {
+  CHECK_CTX(ctx); CHECK_PTR(x_scale); CHECK_PTR(w_scale);
+  UP_REQUIRE(use_tensor_cores(ctx), UNIPOOL_ERR_UNSUPPORTED, "8-bit operands need a bf16 context");
+  return linear_call(ctx, LinearArgs{x, W, x_scale, w_scale, T, n_in, n_out, act, bias, residual, pre, y}, stream);
+}
+
+size_t unipool_linear_bwd_scratch(const unipool_ctx* ctx, int32_t T, int32_t n_in, int32_t n_out) {
+  if (ctx == nullptr || T < 1 || n_in < 64 || n_out < 64 || n_in % 64 != 0 || n_out % 64 != 0) return 0;
+  return linear_bwd_scratch(ctx, T, n_in, n_out);
+}
+
+int unipool_linear_bwd(unipool_ctx* ctx, const void* dy, int32_t T, int32_t n_out, const void* pre, int32_t act,
+                       const void* x, int32_t n_in, const void* W, void* dp, const void* dx_residual, void* dx, float* dW,
+                       float* dbias, void* scratch, int32_t flags, unipool_stream stream) {
+  CHECK_CTX(ctx); CHECK_T(ctx, T); CHECK_FEATURES(n_in); CHECK_FEATURES(n_out); CHECK_ACT(act);
+  CHECK_PTR(dy);
+  if (act != UNIPOOL_ACT_NONE) { CHECK_PTR(pre); CHECK_PTR(dp); }
+  UP_REQUIRE(dx != nullptr || dW != nullptr || dbias != nullptr, UNIPOOL_ERR_INVALID_ARG, "dx, dW and dbias are all NULL");
+  UP_REQUIRE((flags & ~UNIPOOL_WGRAD_OVERWRITE) == 0, UNIPOOL_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
+  if (dx != nullptr) CHECK_PTR(W);
+  if (dW != nullptr) CHECK_PTR(x);
+  if ((dW != nullptr || dbias != nullptr) && T > 0) CHECK_SCRATCH(scratch);
+  CHECK_ALIGNED(ctx, dy); CHECK_ALIGNED(ctx, pre); CHECK_ALIGNED(ctx, dp); CHECK_ALIGNED(ctx, x); CHECK_ALIGNED(ctx, W);
+  CHECK_ALIGNED(ctx, dx_residual); CHECK_ALIGNED(ctx, dx); CHECK_ALIGNED(ctx, dW);
+  LinearBwdArgs a{dy, pre, x, W, T, n_in, n_out, act, dp, dx_residual, dx, dW, dbias, static_cast<float*>(scratch),
+                  (flags & UNIPOOL_WGRAD_OVERWRITE) != 0};
+  return linear_bwd_launch(ctx, a, static_cast<cudaStream_t>(stream));
+}
+
 int unipool_unique_experts(unipool_ctx* ctx, const int32_t* idx, const int32_t* expert_base, int32_t L,
                            int32_t T, int32_t* unique, uint64_t* total, unipool_stream stream) {
   CHECK_CTX(ctx); CHECK_T(ctx, T); CHECK_PTR(idx); CHECK_PTR(unique); CHECK_PTR(total);

@@ -190,6 +190,12 @@ __device__ __forceinline__ float silu_grad_f(float a) {
   return sig * (1.0f + a * (1.0f - sig));
 }
 
+__device__ __forceinline__ float max_nan(float a, float b) {     // NaN if one of them is
+  float m;
+  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
+  return m;
+}
+
 // status codes written by kernels into ws.status[0]
 constexpr int kStatusTimeout = 1;
 constexpr int kStatusCheck = 2;
@@ -233,6 +239,33 @@ size_t rmsnorm_bwd_scratch(const unipool_ctx*, int T, int width);
 int rmsnorm_bwd_launch(unipool_ctx*, const void* dh, const void* r, int T, int width, const float* w, const float* rstd,
                        const void* dr, void* dx, float* dw, float* scratch, bool overwrite, cudaStream_t);
 int quantize_rows_launch(unipool_ctx*, const void* x, int rows, int width, uint8_t* q, float* q_scale, cudaStream_t);
+
+// dense products with an epilogue (linear.cu: the calls and the CUDA-core path; linear_tc.cu: the tensor-core path)
+struct LinearArgs {
+  const void *x, *W;             // [T, n_in], [n_out, n_in]
+  const float *x_scale, *w_scale;   // e4m3 operands: [T], [n_out]; NULL: operands of the ctx dtype
+  int T, n_in, n_out, act;
+  const float* bias;
+  const void* residual;
+  void *pre, *y;
+};
+struct LinearBwdArgs {
+  const void *dy, *pre, *x, *W;
+  int T, n_in, n_out, act;
+  void* dp;                      // [T, n_out] dy act'(pre) (act none: not used)
+  const void* dx_residual;
+  void* dx;
+  float *dW, *dbias, *scratch;
+  bool overwrite;
+};
+int linear_launch(unipool_ctx*, const LinearArgs&, cudaStream_t);
+int linear_bwd_launch(unipool_ctx*, const LinearBwdArgs&, cudaStream_t);
+size_t linear_bwd_scratch(const unipool_ctx*, int T, int n_in, int n_out);
+int linear_fwd_tc(unipool_ctx*, const LinearArgs&, cudaStream_t);
+int linear_dx_tc(unipool_ctx*, const LinearBwdArgs&, const void* dp, cudaStream_t);
+int linear_dw_tc(unipool_ctx*, const LinearBwdArgs&, const void* dp, float* out, int splits, bool add, cudaStream_t);
+int linear_dw_splits_tc(const unipool_ctx*, int T, int n_in, int n_out);
+int column_sum_launch(const float* parts, int n_parts, int64_t width, float* out, bool add, cudaStream_t);
 
 // grouped GEMMs: CUDA-core path (fp32 mode) and tcgen05 path (bf16 mode)
 struct ExpertFwdArgs {

@@ -949,17 +949,21 @@ struct TcModule {
 //   kMapOperand   bf16, 128-byte swizzle (MMA operand tiles)
 //   kMapBf16Chunk bf16, 64-byte swizzle  (32 x 32 epilogue chunks)
 //   kMapF32Chunk  fp32, 128-byte swizzle (32 x 32 epilogue chunks of the weight gradient)
+//   kMapByteOperand  8-bit values, 128-byte swizzle (MMA operand tiles)
 int make_tmap(const unipool_ctx* ctx, CUtensorMap* out, MapKind kind, const void* base, int rank,
               const uint64_t* dims, const uint64_t* strides_elems, const uint32_t* box) {
   const TcModule* mod = static_cast<const TcModule*>(ctx->tmap_cache);
-  const uint64_t esz = kind == kMapF32Chunk ? 4 : 2;
+  const uint64_t esz = kind == kMapF32Chunk ? 4 : kind == kMapByteOperand ? 1 : 2;
   cuuint64_t gdims[3], gstrides[2];
   cuuint32_t gbox[3], estr[3] = {1, 1, 1};
   for (int i = 0; i < rank; ++i) { gdims[i] = dims[i]; gbox[i] = box[i]; }
   for (int i = 0; i + 1 < rank; ++i) gstrides[i] = strides_elems[i] * esz;
   UP_REQUIRE((reinterpret_cast<uintptr_t>(base) & 15) == 0, UNIPOOL_ERR_INVALID_ARG,
              "tensor base %p is not 16-byte aligned", base);
-  CUresult r = mod->encode(out, kind == kMapF32Chunk ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16,
+  const CUtensorMapDataType type = kind == kMapF32Chunk      ? CU_TENSOR_MAP_DATA_TYPE_FLOAT32
+                                   : kind == kMapByteOperand ? CU_TENSOR_MAP_DATA_TYPE_UINT8
+                                                             : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16;
+  CUresult r = mod->encode(out, type,
                            (cuuint32_t)rank, const_cast<void*>(base), gdims, gstrides, gbox, estr,
                            CU_TENSOR_MAP_INTERLEAVE_NONE,
                            kind == kMapBf16Chunk ? CU_TENSOR_MAP_SWIZZLE_64B : CU_TENSOR_MAP_SWIZZLE_128B,

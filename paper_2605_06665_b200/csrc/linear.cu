@@ -1,0 +1,355 @@
+// Dense products with an epilogue and their backward pass: the calls, the fp32 path on CUDA cores, and the element-wise
+// kernels beside both paths.
+//   forward   p = x W^T + bias,  y = act(p) + residual
+//   backward  dp = dy act'(p),  dx = dp W (+ dx_residual),  dW (+)= dp^T x,  dbias (+)= sum_t dp
+#include <type_traits>
+
+#include "common.cuh"
+#include "linear_act.cuh"
+#include "simt_gemm.cuh"
+
+namespace unipool {
+
+namespace {
+
+// ---------------------------------------------------------------- dp and the sums for dbias
+// dp = dy act'(p), rounded to the element type, and the column sums of the unrounded dp over the block's rows, into parts
+// [gridDim.y, N] (one row block: the gradient itself).  A thread owns V columns and every eighth row of the block's run;
+// eight rows' threads are added up in their order.  Bound by HBM (dy, p in, dp out).
+constexpr int kDpRows = 8;                               // rows a block has in hand at a time
+
+template <typename E, int V> struct Row;                 // V consecutive elements
+template <> struct Row<__nv_bfloat16, 8> {
+  static __device__ __forceinline__ void load(const __nv_bfloat16* p, float (&v)[8]) {
+    const uint4 r = __ldg(reinterpret_cast<const uint4*>(p));
+    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(w[i] << 16);
+      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
+    }
+  }
+  static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&v)[8]) {
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
+      w[i] = *reinterpret_cast<const uint32_t*>(&b);
+    }
+    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
+  }
+};
+template <> struct Row<float, 4> {
+  static __device__ __forceinline__ void load(const float* p, float (&v)[4]) {
+    const float4 r = __ldg(reinterpret_cast<const float4*>(p));
+    v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w;
+  }
+  static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
+    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+  }
+};
+template <> struct Row<float, 1> {
+  static __device__ __forceinline__ void load(const float* p, float (&v)[1]) { v[0] = __ldg(p); }
+  static __device__ __forceinline__ void store(float* p, const float (&v)[1]) { *p = v[0]; }
+};
+
+struct DpParams {
+  const void *dy, *p;
+  void* dp;
+  float* parts;
+  int T, N, rows, act;                                   // rows: of a block's run
+  bool add;                                              // one row block: dbias +=
+};
+
+template <typename E, int V, bool kFast>
+__global__ void __launch_bounds__(256) linear_dp_kernel(DpParams a) {
+  grid_wait(a.dy, a.p);
+  __shared__ float s[kDpRows][32 * V];
+  const int g = threadIdx.x / 32, lane = threadIdx.x % 32, c = (blockIdx.x * 32 + lane) * V;
+  const int t0 = blockIdx.y * a.rows, t1 = min(a.T, t0 + a.rows);
+  float sum[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) sum[j] = 0.f;
+  if (c < a.N) {
+#pragma unroll 4
+    for (int t = t0 + g; t < t1; t += kDpRows) {
+      const int64_t at = (int64_t)t * a.N + c;
+      float d[V], p[V];
+      Row<E, V>::load(static_cast<const E*>(a.dy) + at, d);
+      if (a.dp != nullptr) {
+        Row<E, V>::load(static_cast<const E*>(a.p) + at, p);
+#pragma unroll
+        for (int j = 0; j < V; ++j) d[j] *= act_slope<kFast>(p[j], a.act);
+        Row<E, V>::store(static_cast<E*>(a.dp) + at, d);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[j] += d[j];
+    }
+  }
+  if (a.parts == nullptr) return;
+#pragma unroll
+  for (int j = 0; j < V; ++j) s[g][j * 32 + lane] = sum[j];
+  __syncthreads();
+  for (int i = threadIdx.x; i < 32 * V; i += 256) {
+    const int col = (blockIdx.x * 32 + i % 32) * V + i / 32;
+    if (col >= a.N) continue;
+    float v = s[0][i];
+#pragma unroll
+    for (int q = 1; q < kDpRows; ++q) v += s[q][i];
+    float* out = a.parts + (int64_t)blockIdx.y * a.N + col;
+    *out = a.add ? *out + v : v;
+  }
+}
+
+// Row blocks of the kernel: so many that four blocks lie on an SM, of 32 rows at least.
+int dp_row_blocks(const unipool_ctx* ctx, int T, int N, int cols_per_block) {
+  const int across = (N + cols_per_block - 1) / cols_per_block;
+  int n = 4 * ctx->sm_count / across;
+  if (n > (T + 31) / 32) n = (T + 31) / 32;
+  if (n < 1) n = 1;
+  const int rows = (T + n - 1) / n;
+  return (T + rows - 1) / rows;
+}
+
+// ---------------------------------------------------------------- sums of parts, in their order
+// out (+)= sum over the parts.  Few parts of many columns (a weight gradient's): a thread sums four columns, 16 bytes at a time.
+__global__ void __launch_bounds__(256) part_sum_kernel(const float* parts, int n_parts, int64_t width, float* out, bool add) {
+  grid_wait(parts);
+  const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  if (c >= width) return;
+  float4 v = __ldg(reinterpret_cast<const float4*>(parts + c));
+#pragma unroll 4
+  for (int i = 1; i < n_parts; ++i) {
+    const float4 o = __ldg(reinterpret_cast<const float4*>(parts + i * width + c));
+    v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+  }
+  if (add) {
+    out[c] += v.x; out[c + 1] += v.y; out[c + 2] += v.z; out[c + 3] += v.w;
+  } else {
+    out[c] = v.x; out[c + 1] = v.y; out[c + 2] = v.z; out[c + 3] = v.w;
+  }
+}
+// Many parts of few columns: 32 columns to a block, its eight warps take every eighth part.
+__global__ void __launch_bounds__(256) column_sum_kernel(const float* parts, int n_parts, int64_t width, float* out, bool add) {
+  grid_wait(parts);
+  __shared__ float s[8][32];
+  const int g = threadIdx.x / 32;
+  const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x % 32;
+  float v = 0.f;
+  if (c < width) {
+#pragma unroll 8
+    for (int i = g; i < n_parts; i += 8) v += __ldg(parts + i * width + c);
+  }
+  s[g][threadIdx.x % 32] = v;
+  __syncthreads();
+  if (g != 0 || c >= width) return;
+#pragma unroll
+  for (int i = 1; i < 8; ++i) v += s[i][threadIdx.x];
+  out[c] = add ? out[c] + v : v;
+}
+
+// ---------------------------------------------------------------- fp32 products on CUDA cores
+struct SimtLinear {
+  const float *A, *B;
+  float *C, *P;                                          // P: the value before the activation, or NULL
+  const float *bias, *residual;
+  int M, N, K, act;                                      // C [M, N]
+  int k_len;                                             // dW: tokens of a part
+  bool vec_a, vec_b, vec_c, add;                         // 16-byte aligned operands; vec_c: everything of the epilogue
+};
+
+// C = act(A B + bias) + residual; B along K (forward) or across it (dx).
+template <typename Tile, Major BM>
+__global__ void __launch_bounds__(Tile::kThreads, Tile::kBlocks) linear_rows_kernel(SimtLinear p) {
+  grid_wait(p.A, p.B, p.bias, p.residual);
+  extern __shared__ float4 smem_raw[];
+  typename Tile::Smem& sm = *reinterpret_cast<typename Tile::Smem*>(smem_raw);
+  const int m0 = blockIdx.x * Tile::kRows, n0 = blockIdx.y * kSimtN;
+  Tile t;
+  t.template run<kAlongK, BM>(
+      sm, p.K / kSimtKC, p.vec_a, p.vec_b, p.A, [](int) {},
+      [&](int c, int i, int k) { return m0 + i < p.M ? p.A + (int64_t)(m0 + i) * p.K + c * kSimtKC + k : nullptr; },
+      [&](int c, int i, int k) {
+        return BM == kAlongK ? p.B + (int64_t)(n0 + i) * p.K + c * kSimtKC + k : p.B + (int64_t)(c * kSimtKC + k) * p.N + n0 + i;
+      });
+  t.each4(sm, [&](int i, int j, float4 v) {
+    if (m0 + i >= p.M) return;
+    const int n = n0 + j;
+    const int64_t at = (int64_t)(m0 + i) * p.N + n;
+    if (p.bias != nullptr) {
+      const float4 b = ld4(p.bias + n, p.vec_c);
+      v = make_float4(v.x + b.x, v.y + b.y, v.z + b.z, v.w + b.w);
+    }
+    if (p.P != nullptr) st4(p.P + at, v, p.vec_c);
+    v = make_float4(act_value<false>(v.x, p.act), act_value<false>(v.y, p.act), act_value<false>(v.z, p.act),
+                    act_value<false>(v.w, p.act));
+    if (p.residual != nullptr) {
+      // (C may be the residual itself: a thread's own elements, and no read-only load)
+      const float* r = p.residual + at;
+      const float4 b = p.vec_c ? *reinterpret_cast<const float4*>(r) : make_float4(r[0], r[1], r[2], r[3]);
+      v = make_float4(v.x + b.x, v.y + b.y, v.z + b.z, v.w + b.w);
+    }
+    st4(p.C + at, v, p.vec_c);
+  });
+}
+
+// C [M, N] (+)= sum over the tokens of a part of A[t, m] B[t, n]; part z of C behind the one before it.
+using LinearDwTile = SimtBlockTile<2>;
+__global__ void __launch_bounds__(LinearDwTile::kThreads, LinearDwTile::kBlocks) linear_dw_kernel(SimtLinear p) {
+  grid_wait(p.A, p.B);
+  extern __shared__ float4 smem_raw[];
+  LinearDwTile::Smem& sm = *reinterpret_cast<LinearDwTile::Smem*>(smem_raw);
+  const int m0 = blockIdx.x * LinearDwTile::kRows, n0 = blockIdx.y * kSimtN;
+  const int k0 = blockIdx.z * p.k_len, k1 = min(p.K, k0 + p.k_len);
+  LinearDwTile t;
+  t.run<kAcrossK, kAcrossK>(
+      sm, (k1 - k0 + kSimtKC - 1) / kSimtKC, p.vec_a, p.vec_b, p.A, [](int) {},
+      [&](int c, int i, int k) -> const float* {
+        const int tok = k0 + c * kSimtKC + k;
+        return tok < k1 ? p.A + (int64_t)tok * p.M + m0 + i : nullptr;
+      },
+      [&](int c, int i, int k) -> const float* {
+        const int tok = k0 + c * kSimtKC + k;
+        return tok < k1 ? p.B + (int64_t)tok * p.N + n0 + i : nullptr;
+      });
+  t.each4(sm, [&](int i, int j, float4 v) {
+    float* o = p.C + ((int64_t)blockIdx.z * p.M + m0 + i) * p.N + n0 + j;
+    if (p.add) v = make_float4(v.x + o[0], v.y + o[1], v.z + o[2], v.w + o[3]);
+    st4(o, v, p.vec_c);
+  });
+}
+
+template <typename Tile, Major BM> int rows_as(unipool_ctx* ctx, int phase, const SimtLinear& p, cudaStream_t s) {
+  PhaseTimer pt(ctx, phase, 1, s);
+  auto kern = linear_rows_kernel<Tile, BM>;
+  constexpr int smem = (int)sizeof(typename Tile::Smem);
+  UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
+  UP_KERNEL(kern, dim3((p.M + Tile::kRows - 1) / Tile::kRows, p.N / kSimtN), Tile::kThreads, smem, s, p);
+  return UNIPOOL_OK;
+}
+template <Major BM> int rows_simt(unipool_ctx* ctx, int phase, const SimtLinear& p, cudaStream_t s) {
+  const int64_t tiles = (int64_t)((p.M + kSimtM - 1) / kSimtM) * (p.N / kSimtN);
+  if (tiles <= ctx->sm_count) return rows_as<SimtTile<8>, BM>(ctx, phase, p, s);
+  if (tiles <= 6 * ctx->sm_count) return rows_as<SimtTile<4>, BM>(ctx, phase, p, s);
+  return rows_as<SimtBlockTile<1>, BM>(ctx, phase, p, s);
+}
+
+// Parts of the tokens for the weight gradient: two blocks of tiles to an SM, 256 tokens at least to a part.
+int dw_splits_simt(const unipool_ctx* ctx, int T, int n_in, int n_out) {
+  const int tiles = (n_out / 64) * (n_in / 64);
+  int n = (2 * ctx->sm_count + tiles - 1) / tiles;
+  if (n > (T + 255) / 256) n = (T + 255) / 256;
+  if (n < 1) n = 1;
+  const int len = ((T + n - 1) / n + kSimtKC - 1) / kSimtKC * kSimtKC;
+  return (T + len - 1) / len;
+}
+int dw_simt(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, float* out, int splits, bool add, cudaStream_t s) {
+  SimtLinear p{};
+  p.A = static_cast<const float*>(dp); p.B = static_cast<const float*>(a.x); p.C = out;
+  p.M = a.n_out; p.N = a.n_in; p.K = a.T; p.add = add;
+  p.k_len = ((a.T + splits - 1) / splits + kSimtKC - 1) / kSimtKC * kSimtKC;
+  p.vec_a = aligned16(p.A); p.vec_b = aligned16(p.B); p.vec_c = aligned16(p.C);
+  PhaseTimer pt(ctx, UNIPOOL_PH_LINEAR_BWD, 1, s);
+  UP_CUDA(cudaFuncSetAttribute(linear_dw_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(LinearDwTile::Smem)));
+  UP_KERNEL(linear_dw_kernel, dim3(a.n_out / LinearDwTile::kRows, a.n_in / kSimtN, splits), LinearDwTile::kThreads,
+            sizeof(LinearDwTile::Smem), s, p);
+  return UNIPOOL_OK;
+}
+
+bool tensor_cores(const unipool_ctx* ctx) { return ctx->cfg.dtype == UNIPOOL_BF16; }
+int dw_splits(const unipool_ctx* ctx, int T, int n_in, int n_out) {
+  return tensor_cores(ctx) ? linear_dw_splits_tc(ctx, T, n_in, n_out) : dw_splits_simt(ctx, T, n_in, n_out);
+}
+
+template <typename E, int V, bool kFast>
+int dp_as(unipool_ctx* ctx, const LinearBwdArgs& a, int* blocks, float* parts, cudaStream_t s) {
+  const int n = dp_row_blocks(ctx, a.T, a.n_out, 32 * V);
+  DpParams p{a.dy, a.pre, a.act != UNIPOOL_ACT_NONE ? a.dp : nullptr, nullptr, a.T, a.n_out, (a.T + n - 1) / n, a.act, false};
+  if (a.dbias != nullptr) {
+    p.parts = n > 1 ? parts : a.dbias;
+    p.add = n == 1 && !a.overwrite;
+  }
+  PhaseTimer pt(ctx, UNIPOOL_PH_LINEAR_BWD, 1, s);
+  UP_KERNEL((linear_dp_kernel<E, V, kFast>), dim3((a.n_out + 32 * V - 1) / (32 * V), n), 256, 0, s, p);
+  *blocks = n;
+  return UNIPOOL_OK;
+}
+
+}  // namespace
+
+int column_sum_launch(const float* parts, int n_parts, int64_t width, float* out, bool add, cudaStream_t s) {
+  // Few columns: every block's eight warps share the parts; many: each thread walks over them with 16-byte loads.
+  if (width % 4 == 0 && width >= 4 * 256 * 148 && aligned16(parts))
+    UP_KERNEL(part_sum_kernel, (unsigned)((width / 4 + 255) / 256), 256, 0, s, parts, n_parts, width, out, add);
+  else
+    UP_KERNEL(column_sum_kernel, (unsigned)((width + 31) / 32), 256, 0, s, parts, n_parts, width, out, add);
+  return UNIPOOL_OK;
+}
+
+int linear_launch(unipool_ctx* ctx, const LinearArgs& a, cudaStream_t s) {
+  if (a.T == 0) return UNIPOOL_OK;
+  if (tensor_cores(ctx)) return linear_fwd_tc(ctx, a, s);
+  SimtLinear p{};
+  p.A = static_cast<const float*>(a.x); p.B = static_cast<const float*>(a.W); p.C = static_cast<float*>(a.y);
+  p.P = static_cast<float*>(a.pre); p.bias = a.bias; p.residual = static_cast<const float*>(a.residual);
+  p.M = a.T; p.N = a.n_out; p.K = a.n_in; p.act = a.act;
+  p.vec_a = aligned16(p.A); p.vec_b = aligned16(p.B); p.vec_c = aligned16(p.C, p.P, p.bias, p.residual);
+  return rows_simt<kAlongK>(ctx, UNIPOOL_PH_LINEAR, p, s);
+}
+
+// Scratch: the parts of dW, then those of dbias.
+static size_t dw_parts(const unipool_ctx* ctx, int T, int n_in, int n_out) {
+  const int splits = dw_splits(ctx, T, n_in, n_out);
+  return splits > 1 ? (size_t)splits * n_in * n_out : 0;
+}
+size_t linear_bwd_scratch(const unipool_ctx* ctx, int T, int n_in, int n_out) {
+  const int n = dp_row_blocks(ctx, T, n_out, 32 * (tensor_cores(ctx) ? 8 : 4)), m = dp_row_blocks(ctx, T, n_out, 32);
+  return (dw_parts(ctx, T, n_in, n_out) + (size_t)(n > m ? n : m) * n_out) * sizeof(float);
+}
+
+int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) {
+  if (a.T == 0) {
+    if (a.overwrite && a.dW != nullptr) UP_CUDA(cudaMemsetAsync(a.dW, 0, (size_t)a.n_in * a.n_out * sizeof(float), s));
+    if (a.overwrite && a.dbias != nullptr) UP_CUDA(cudaMemsetAsync(a.dbias, 0, (size_t)a.n_out * sizeof(float), s));
+    return UNIPOOL_OK;
+  }
+  const bool tc = tensor_cores(ctx), act = a.act != UNIPOOL_ACT_NONE;
+  const void* dp = act ? a.dp : a.dy;
+  int rc = UNIPOOL_OK;
+  if (act || a.dbias != nullptr) {
+    float* parts = a.scratch ? a.scratch + dw_parts(ctx, a.T, a.n_in, a.n_out) : nullptr;
+    int blocks = 1;
+    rc = tc ? dp_as<__nv_bfloat16, 8, true>(ctx, a, &blocks, parts, s)
+         : aligned16(a.dy, a.pre, act ? a.dp : nullptr) ? dp_as<float, 4, false>(ctx, a, &blocks, parts, s)
+                                                        : dp_as<float, 1, false>(ctx, a, &blocks, parts, s);
+    if (rc != UNIPOOL_OK) return rc;
+    if (a.dbias != nullptr && blocks > 1) {
+      PhaseTimer pt(ctx, UNIPOOL_PH_LINEAR_BWD, 1, s);
+      rc = column_sum_launch(parts, blocks, a.n_out, a.dbias, !a.overwrite, s);
+      if (rc != UNIPOOL_OK) return rc;
+    }
+  }
+  if (a.dx != nullptr) {
+    if (tc) {
+      rc = linear_dx_tc(ctx, a, dp, s);
+    } else {
+      SimtLinear p{};
+      p.A = static_cast<const float*>(dp); p.B = static_cast<const float*>(a.W); p.C = static_cast<float*>(a.dx);
+      p.residual = static_cast<const float*>(a.dx_residual);
+      p.M = a.T; p.N = a.n_in; p.K = a.n_out; p.act = UNIPOOL_ACT_NONE;
+      p.vec_a = aligned16(p.A); p.vec_b = aligned16(p.B); p.vec_c = aligned16(p.C, p.residual);
+      rc = rows_simt<kAcrossK>(ctx, UNIPOOL_PH_LINEAR_BWD, p, s);
+    }
+    if (rc != UNIPOOL_OK) return rc;
+  }
+  if (a.dW == nullptr) return UNIPOOL_OK;
+  const int splits = dw_splits(ctx, a.T, a.n_in, a.n_out);
+  float* out = splits > 1 ? a.scratch : a.dW;
+  const bool add = splits == 1 && !a.overwrite;
+  rc = tc ? linear_dw_tc(ctx, a, dp, out, splits, add, s) : dw_simt(ctx, a, dp, out, splits, add, s);
+  if (rc != UNIPOOL_OK || splits == 1) return rc;
+  PhaseTimer pt(ctx, UNIPOOL_PH_LINEAR_BWD, 1, s);
+  return column_sum_launch(a.scratch, splits, (int64_t)a.n_in * a.n_out, a.dW, !a.overwrite, s);
+}
+
+}  // namespace unipool

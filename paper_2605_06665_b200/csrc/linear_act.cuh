@@ -1,0 +1,43 @@
+// Activations of the dense products and their derivatives.  kFast: through the special-function unit (errors of a few
+// 2^-22, far below the rounding to bf16); otherwise CUDA's expf and divisions.
+#pragma once
+
+#include "common.cuh"
+
+namespace unipool {
+
+template <bool kFast> __device__ __forceinline__ float logistic(float a) {
+  if constexpr (kFast) return __fdividef(1.f, 1.f + __expf(-a));
+  else return 1.f / (1.f + expf(-a));
+}
+
+// gelu (tanh form): 0.5 p (1 + tanh(u)) = p logistic(2 u), u = sqrt(2 / pi) (p + 0.044715 p^3); as a product with the
+// logistic function it keeps its relative accuracy where the tanh nears -1.
+constexpr float kGeluTwice = 1.5957691216057308f, kGeluCube = 0.044715f;
+
+template <bool kFast> __device__ __forceinline__ float act_value(float p, int act) {
+  switch (act) {
+    case UNIPOOL_ACT_RELU: return max_nan(p, 0.f);
+    case UNIPOOL_ACT_SILU: return p * logistic<kFast>(p);
+    case UNIPOOL_ACT_GELU: return p * logistic<kFast>(kGeluTwice * (p + kGeluCube * p * p * p));
+    default: return p;
+  }
+}
+
+template <bool kFast> __device__ __forceinline__ float act_slope(float p, int act) {
+  switch (act) {
+    case UNIPOOL_ACT_RELU: return p > 0.f ? 1.f : p <= 0.f ? 0.f : p;
+    case UNIPOOL_ACT_SILU: {
+      const float s = logistic<kFast>(p);
+      return s * (1.f + p * (1.f - s));
+    }
+    case UNIPOOL_ACT_GELU: {
+      const float q = p > 30.f ? 30.f : p < -30.f ? -30.f : p;      // 0 or 1 from there on; the square would overflow
+      const float s = logistic<kFast>(kGeluTwice * (q + kGeluCube * q * q * q));
+      return s + q * s * (1.f - s) * kGeluTwice * (1.f + 3.f * kGeluCube * q * q);
+    }
+    default: return 1.f;
+  }
+}
+
+}  // namespace unipool

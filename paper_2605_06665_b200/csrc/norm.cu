@@ -23,12 +23,6 @@ constexpr int kNormMaxWidth = 16384;
 constexpr float kE4m3Max = 448.f;
 constexpr float kSmallestScale = 1.17549435e-38f;        // 2^-126: its reciprocal is finite, a row of zeros keeps zeros
 
-__device__ __forceinline__ float max_nan(float a, float b) {     // NaN if one of them is
-  float m;
-  asm("max.NaN.f32 %0, %1, %2;" : "=f"(m) : "f"(a), "f"(b));
-  return m;
-}
-
 // V consecutive elements as they lie in memory: 16 bytes, or a single element where those do not fit.
 template <typename E, int V> struct Vec;
 template <> struct Vec<__nv_bfloat16, 8> {
@@ -312,22 +306,6 @@ __global__ void __launch_bounds__(kNormBwdThreads<TPR>) rmsnorm_bwd_kernel(NormB
   }
 }
 
-// dw (+)= the blocks' sums, in their order: 32 columns to a block, its eight warps take every eighth of the sums.
-__global__ void __launch_bounds__(256) column_sum_kernel(const float* parts, int n_parts, int width, float* out, bool add) {
-  grid_wait(parts);
-  __shared__ float s[8][32];
-  const int g = threadIdx.x / 32, c = blockIdx.x * 32 + threadIdx.x % 32;
-  float v = 0.f;
-  if (c < width)
-    for (int i = g; i < n_parts; i += 8) v += __ldg(parts + (int64_t)i * width + c);
-  s[g][threadIdx.x % 32] = v;
-  __syncthreads();
-  if (g != 0 || c >= width) return;
-#pragma unroll
-  for (int i = 1; i < 8; ++i) v += s[i][threadIdx.x];
-  out[c] = add ? out[c] + v : v;
-}
-
 // Calls f(TPR, VPT) as compile-time numbers for rows of `n` vectors.
 template <int N> using Int = std::integral_constant<int, N>;
 template <bool kScalar, typename F> int by_width(int n, F f) {
@@ -390,8 +368,7 @@ template <typename E> int norm_bwd_as(unipool_ctx* ctx, NormBwdParams p, float* 
     PhaseTimer pt(ctx, UNIPOOL_PH_RMSNORM_BWD, split ? 2 : 1, s);
     auto kern = rmsnorm_bwd_kernel<decltype(e), v, tpr, vpt>;
     UP_KERNEL(kern, blocks, kNormBwdThreads<tpr>, tpr == 32 ? p.width * sizeof(float) : 0, s, a);
-    if (split) UP_KERNEL(column_sum_kernel, (p.width + 31) / 32, 256, 0, s, scratch, blocks, p.width, dw, !overwrite);
-    return UNIPOOL_OK;
+    return split ? column_sum_launch(scratch, blocks, p.width, dw, !overwrite, s) : UNIPOOL_OK;
   });
 }
 

@@ -17,7 +17,7 @@ enum Mode : int {
 
 constexpr int kWmMaxExperts = 400;        // experts of a launch of the weights-on-M kernels (their shared-memory table)
 
-enum MapKind { kMapOperand, kMapBf16Chunk, kMapF32Chunk };
+enum MapKind { kMapOperand, kMapBf16Chunk, kMapF32Chunk, kMapByteOperand };
 int make_tmap(const unipool_ctx* ctx, CUtensorMap* out, MapKind kind, const void* base, int rank,
               const uint64_t* dims, const uint64_t* strides_elems, const uint32_t* box);
 int map_2d(const unipool_ctx* ctx, CUtensorMap* out, const void* base, uint64_t cols, uint64_t rows,

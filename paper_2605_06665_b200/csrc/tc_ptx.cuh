@@ -249,6 +249,16 @@ __device__ __forceinline__ void umma_bf16_pair(uint32_t d_tmem, uint64_t a_desc,
       ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
       : "memory");
 }
+// The same for 8-bit operands (e4m3, K = 32).
+__device__ __forceinline__ void umma_e4m3_pair(uint32_t d_tmem, uint64_t a_desc, uint64_t b_desc, uint32_t idesc,
+                                               uint32_t accumulate) {
+  asm volatile(
+      "{\n\t.reg .pred p;\n\t"
+      "setp.ne.b32 p, %4, 0;\n\t"
+      "tcgen05.mma.cta_group::2.kind::f8f6f4 [%0], %1, %2, %3, p;\n\t}"
+      ::"r"(d_tmem), "l"(a_desc), "l"(b_desc), "r"(idesc), "r"(accumulate)
+      : "memory");
+}
 // Issued where `issue` is nonzero: for a warp that runs its issuing loop as a whole, in the one lane that issues (in a
 // loop of one lane alone the operands are moved to uniform registers for every instruction, some 70 clocks per MMA),
 // and for steps of a k-block that may be left out.
@@ -305,6 +315,11 @@ __host__ __device__ constexpr uint32_t instr_desc_bf16(int n, bool a_mn, bool b_
   return (1u << 4) | (1u << 7) | (1u << 10) | (static_cast<uint32_t>(a_mn) << 15) |
          (static_cast<uint32_t>(b_mn) << 16) | (static_cast<uint32_t>(n >> 3) << 17) |
          (static_cast<uint32_t>(m >> 4) << 24);
+}
+
+// The same for kind::f8f6f4 with e4m3 operands (format 0), both K-major.
+__host__ __device__ constexpr uint32_t instr_desc_e4m3(int n, int m) {
+  return (1u << 4) | (static_cast<uint32_t>(n >> 3) << 17) | (static_cast<uint32_t>(m >> 4) << 24);
 }
 
 }  // namespace tc
