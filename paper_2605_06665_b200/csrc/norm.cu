@@ -280,7 +280,7 @@ __global__ void __launch_bounds__(kNormBwdThreads<TPR>) rmsnorm_bwd_kernel(NormB
     }
   }
   if (p.dw == nullptr) return;
-  float* out = p.dw + (int64_t)blockIdx.x * p.width;
+  float* out = &p.dw[(int64_t)blockIdx.x * p.width];
   if constexpr (TPR == 32) {
     for (int g = 0; g < kRows; ++g) {
       if ((int)threadIdx.x / 32 == g) {
