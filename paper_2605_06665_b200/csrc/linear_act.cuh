@@ -6,8 +6,16 @@
 
 namespace unipool {
 
+// 1 / (1 + 2^z)
+__device__ __forceinline__ float rcp_1_ex2(float z) {
+  float e, r;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(e) : "f"(z));
+  asm("rcp.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(1.f + e));
+  return r;
+}
+constexpr float kLog2e = 1.4426950408889634f;
 template <bool kFast> __device__ __forceinline__ float logistic(float a) {
-  if constexpr (kFast) return __fdividef(1.f, 1.f + __expf(-a));
+  if constexpr (kFast) return rcp_1_ex2(-kLog2e * a);
   else return 1.f / (1.f + expf(-a));
 }
 
@@ -19,7 +27,9 @@ template <bool kFast> __device__ __forceinline__ float act_value(float p, int ac
   switch (act) {
     case UNIPOOL_ACT_RELU: return max_nan(p, 0.f);
     case UNIPOOL_ACT_SILU: return p * logistic<kFast>(p);
-    case UNIPOOL_ACT_GELU: return p * logistic<kFast>(kGeluTwice * (p + kGeluCube * p * p * p));
+    case UNIPOOL_ACT_GELU:
+      if constexpr (kFast) return p * rcp_1_ex2(p * fmaf(p * p, -kLog2e * kGeluTwice * kGeluCube, -kLog2e * kGeluTwice));
+      else return p * logistic<false>(kGeluTwice * (p + kGeluCube * p * p * p));
     default: return p;
   }
 }

@@ -5,9 +5,10 @@
 //
 // linear_pair_kernel: persistent CTA pairs as in the grouped kernels (expert_tc.cu): 256 x 256 tiles, M = 256 over both CTAs'
 // tensor memory, six 32 KB operand stages a CTA, accumulators double-buffered so that a tile's epilogue runs beside the next
-// one's products.  Eight epilogue warps, two to a TMEM lane quarter with 128 columns each: an activation costs two
-// special-function instructions an element, which four warps could not hide behind the products of 768 inputs.
-// The residual comes by TMA into the staging tile that the result leaves from, a chunk of 32 x 32 ahead.
+// one's products.  Sixteen epilogue warps, four to a TMEM lane quarter with 64 columns each: a chunk of 32 x 32 is a chain of
+// waits (tensor memory, shared memory, proxy fence, TMA) of a microsecond, which it takes four warps on a scheduler to hide behind
+// the products of 768 inputs, the special-function unit (two instructions an element of silu and gelu) being busy for 2.2 of
+// the 3.1 us that they take.
 // Bound by the tensor pipe (operands through shared memory; see expert_tc.cu) and, held for long, by power.
 #include <cuda.h>
 
@@ -24,12 +25,12 @@ enum LinearKind { kLinFwd, kLinFwd8, kLinDx, kLinDw };
 
 constexpr uint32_t kLinHalf = 128 * 128;                 // 128 rows (columns) x 128 bytes of one operand
 constexpr uint32_t kLinStage = 2 * kLinHalf;
-constexpr uint32_t kLinBars = 229376;                    // operand stages + staging fill this much
+constexpr uint32_t kLinBars = 229376;                    // operand stages and staging tiles fill this much
 constexpr uint32_t kLinSmem = kLinBars + 512 + 1024;
-constexpr int kLinEpiWarps = 8;
+constexpr int kLinEpiWarps = 16;
 constexpr int kLinThreads = 64 + 32 * kLinEpiWarps;
-constexpr int kLinChunk = 32;
-constexpr uint32_t kLinBf16Chunk = 32 * kLinChunk * 2, kLinF32Chunk = 32 * kLinChunk * 4;
+constexpr int kLinChunk = 32;                            // columns that an epilogue warp has in hand
+constexpr uint32_t kLinTile = 32 * kLinChunk * 2;        // a chunk of 32 rows in bf16, rows of 64 bytes
 // The tensor core truncates the sums it adds to: a sum over K terms loses 1.1e-9 K of itself (measured, 512 to 32768 rows).  The
 // weight gradient, an fp32 result of a sum over all tokens, is therefore taken from the accumulator every 768 tokens and
 // added up in registers, where it is rounded to nearest.
@@ -40,7 +41,12 @@ struct LinearParams {
   int n_mt, n_nt, units, kb_total, kb_split;
   int act;
   const float *bias, *x_scale, *w_scale;
-  bool residual, add, vec;           // vec: bias and w_scale are 16-byte aligned
+  bool pre;                          // the value before the activation is stored too
+  bool vec;                          // bias and w_scale are 16-byte aligned
+  const __nv_bfloat16* residual;     // [M, N] or NULL
+  float* dw;                         // weight gradient: [splits, M, N]
+  bool add;                          // ... +=
+  bool wide;                         // residual, or dw, is 32-byte aligned
   int32_t* status;
 };
 
@@ -65,43 +71,50 @@ __device__ __forceinline__ void linear_timeout(int32_t* status, volatile int* ab
   }
 }
 
-// 16-byte piece q of row r of a staging tile in the layout of the TMA swizzle: rows of 64 bytes, rows of 128.
-__device__ __forceinline__ uint4* piece64(uint8_t* tile, int r, int q) {
-  return reinterpret_cast<uint4*>(tile + r * 64 + ((q ^ ((r >> 1) & 3)) << 4));
+// 32 bytes at p, a sector (`wide`: p is 32-byte aligned, else 16).
+__device__ __forceinline__ void st_sector(void* p, const uint32_t* v, bool wide) {
+  if (wide) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+  } else {
+    static_cast<uint4*>(p)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+    static_cast<uint4*>(p)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+  }
 }
-__device__ __forceinline__ uint4* piece128(uint8_t* tile, int r, int q) {
-  return reinterpret_cast<uint4*>(tile + r * 128 + ((q ^ (r & 7)) << 4));
+__device__ __forceinline__ void ld_sector(const void* p, uint32_t* v, bool wide) {
+  if (wide) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(v[0]), "=r"(v[1]), "=r"(v[2]), "=r"(v[3]), "=r"(v[4]), "=r"(v[5]), "=r"(v[6]), "=r"(v[7])
+                 : "l"(p)
+                 : "memory");
+  } else {
+    const uint4 a = static_cast<const uint4*>(p)[0], b = static_cast<const uint4*>(p)[1];
+    v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
+    v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
+  }
+}
+// 16-byte piece q of row r of a staging tile in the layout of the 64-byte TMA swizzle
+__device__ __forceinline__ uint4* piece(uint8_t* tile, int r, int q) {
+  return reinterpret_cast<uint4*>(tile + r * 64 + ((q ^ ((r >> 1) & 3)) << 4));
 }
 __device__ __forceinline__ void put_row(uint8_t* tile, int r, const float (&v)[32]) {
 #pragma unroll
   for (int q = 0; q < 4; ++q)
-    *piece64(tile, r, q) = make_uint4(tc::pack_bf16(v[8 * q], v[8 * q + 1]), tc::pack_bf16(v[8 * q + 2], v[8 * q + 3]),
-                                      tc::pack_bf16(v[8 * q + 4], v[8 * q + 5]), tc::pack_bf16(v[8 * q + 6], v[8 * q + 7]));
+    *piece(tile, r, q) = make_uint4(tc::pack_bf16(v[8 * q], v[8 * q + 1]), tc::pack_bf16(v[8 * q + 2], v[8 * q + 3]),
+                                    tc::pack_bf16(v[8 * q + 4], v[8 * q + 5]), tc::pack_bf16(v[8 * q + 6], v[8 * q + 7]));
 }
-__device__ __forceinline__ void add_row(uint8_t* tile, int r, float (&v)[32]) {
+// 32 consecutive values, the same in all lanes
+struct Columns {
+  float4 v[8];
+  __device__ __forceinline__ void load(const float* p, bool vec) {
 #pragma unroll
-  for (int q = 0; q < 4; ++q) {
-    const uint4 w = *piece64(tile, r, q);
-    const uint32_t ww[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[8 * q + 2 * i] += __uint_as_float(ww[i] << 16);
-      v[8 * q + 2 * i + 1] += __uint_as_float(ww[i] & 0xffff0000u);
-    }
+    for (int q = 0; q < 8; ++q)
+      v[q] = vec ? __ldg(reinterpret_cast<const float4*>(p) + q)
+                 : make_float4(__ldg(p + 4 * q), __ldg(p + 4 * q + 1), __ldg(p + 4 * q + 2), __ldg(p + 4 * q + 3));
   }
-}
-// v = f(v, column's number) for the 32 columns from `p` on, the same in all lanes
-template <typename F> __device__ __forceinline__ void by_column(const float* p, bool vec, float (&v)[32], F f) {
-#pragma unroll
-  for (int q = 0; q < 8; ++q) {
-    const float4 b = vec ? __ldg(reinterpret_cast<const float4*>(p) + q)
-                         : make_float4(__ldg(p + 4 * q), __ldg(p + 4 * q + 1), __ldg(p + 4 * q + 2), __ldg(p + 4 * q + 3));
-    v[4 * q] = f(v[4 * q], b.x);
-    v[4 * q + 1] = f(v[4 * q + 1], b.y);
-    v[4 * q + 2] = f(v[4 * q + 2], b.z);
-    v[4 * q + 3] = f(v[4 * q + 3], b.w);
-  }
-}
+  __device__ __forceinline__ float at(int i) const { return i % 4 == 0 ? v[i / 4].x : i % 4 == 1 ? v[i / 4].y : i % 4 == 2 ? v[i / 4].z : v[i / 4].w; }
+};
 __device__ __forceinline__ void activate(float (&v)[32], int act) {
 #define UP_ACT(a)                                                          \
   case a:                                                                  \
@@ -115,15 +128,17 @@ __device__ __forceinline__ void activate(float (&v)[32], int act) {
 #undef UP_ACT
 }
 
-// kPre: the value before the activation is stored too; two more staging tiles a warp take an operand stage.
-template <int KIND, bool kPre>
+// kRes: a residual is added.  All of it is asked for before the accumulator is waited for: the first chunk's comes by TMA into
+// the staging tile, the second's into registers (a second tile for it would take an operand stage: 16384 tokens, 2048 -> 768 48.7
+// us instead of XX).  kPre: the value before the activation is stored too (one kernel with and without it where no residual is).
+template <int KIND, bool kRes, bool kPre>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                    const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmR,
                    const __grid_constant__ CUtensorMap tmP, LinearParams p) {
-  constexpr int kStages = kPre ? 5 : 6;
-  constexpr uint32_t kStaging = (kLinBars - kStages * kLinStage) / kLinEpiWarps;
-  static_assert(kStaging >= (kPre ? 4 : 2) * kLinBf16Chunk && kStaging >= kLinF32Chunk, "staging tiles");
+  constexpr int kStages = KIND == kLinDw ? 7 : 6;
+  constexpr uint32_t kStaging = KIND == kLinDw ? 0 : kLinTile;
+  static_assert(kStages * kLinStage + kLinEpiWarps * kStaging == kLinBars, "shared memory");
   constexpr bool kAMn = KIND == kLinDw, kBMn = KIND == kLinDx || KIND == kLinDw;
   constexpr int kKb = KIND == kLinFwd8 ? 128 : 64;       // elements of a k-block
   extern __shared__ uint8_t smem_raw[];
@@ -132,10 +147,10 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   uint64_t* empty_bar = full_bar + kStages;
   uint64_t* tmem_full = empty_bar + kStages;
   uint64_t* tmem_empty = tmem_full + 2;
-  uint64_t* res_bar = tmem_empty + 2;                    // [8][2] a chunk of the residual has landed
-  uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(res_bar + 2 * kLinEpiWarps);
+  uint64_t* res_bar = tmem_empty + 2;                    // [16] a chunk of the residual has landed
+  uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(res_bar + (kRes ? kLinEpiWarps : 0));
   volatile int* abort = reinterpret_cast<volatile int*>(tmem_ptr + 1);
-  static_assert((2 * kStages + 4 + 2 * kLinEpiWarps) * 8 + 8 <= 512, "barrier block");
+  static_assert((2 * kStages + 4 + kLinEpiWarps) * 8 + 8 <= 512, "barrier block");
 
   const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
   const int rank = (int)tc::cluster_ctarank();           // 0 = leader
@@ -144,12 +159,12 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   if (threadIdx.x == 0) {
     for (int s = 0; s < kStages; ++s) { tc::mbar_init(&full_bar[s], 1); tc::mbar_init(&empty_bar[s], 1); }
     for (int a = 0; a < 2; ++a) { tc::mbar_init(&tmem_full[a], 1); tc::mbar_init(&tmem_empty[a], 2 * kLinEpiWarps); }
-    for (int i = 0; i < 2 * kLinEpiWarps; ++i) tc::mbar_init(&res_bar[i], 1);
+    if constexpr (kRes)
+      for (int i = 0; i < kLinEpiWarps; ++i) tc::mbar_init(&res_bar[i], 1);
     *abort = 0;
     tc::fence_barrier_init();
     tc::tma_prefetch_desc(&tmA);
     tc::tma_prefetch_desc(&tmB);
-    tc::tma_prefetch_desc(&tmC);
   }
   if (warp == 1) {
     tc::tmem_alloc_pair(tmem_ptr, 512);
@@ -160,7 +175,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   tc::cluster_sync();                                    // both CTAs' barriers exist before any remote use
   tc::tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_ptr;
-  grid_wait(p.bias, p.x_scale, p.w_scale);
+  grid_wait(p.bias, p.x_scale, p.w_scale, p.residual);
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (one in each CTA)
@@ -224,13 +239,12 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       }
     }
   } else {
-    // ------------------------------------------------------------ epilogue: 32 rows and 128 columns of the tile to a warp
-    const int quarter = warp & 3, ew = warp - 2, half = ew >> 2;
+    // ------------------------------------------------------------ epilogue: 32 rows and 64 columns of the tile to a warp
+    const int quarter = warp & 3, ew = warp - 2, part = ew >> 2;
     uint8_t* stg = smem + kStages * kLinStage + ew * kStaging;
-    uint64_t* my_res = res_bar + 2 * ew;
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
     int local = 0;
-    uint32_t chunk = 0, loaded = 0;                       // chunks staged, chunks of the residual asked for
+    uint32_t turn = 0;                                    // chunks of the residual that have landed in the staging tile
     bool ok = true;
     auto release = [&](int acc) {
       tc::tc_fence_before_sync();
@@ -249,109 +263,148 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     };
     for (int u = pair; u < p.units && ok; u += n_pairs) {
       const LinearUnit t = linear_unit(p, u);
-      const int row0 = t.mt * 256 + rank * 128 + quarter * 32, col0 = t.nt * 256 + half * 128;
-      const int nch = row0 < p.M ? max(0, min(4, (p.N - col0 + kLinChunk - 1) / kLinChunk)) : 0;
+      const int row0 = t.mt * 256 + rank * 128 + quarter * 32, col0 = t.nt * 256 + part * 64;
+      const int nch = row0 < p.M ? max(0, min(2, (p.N - col0) / kLinChunk)) : 0;
       if constexpr (KIND == kLinDw) {
-        float sum[4][32];
-        for (int kb = t.kb0, first = 1; kb < t.kb1 && ok; kb += kLinSegment, first = 0) {
+        float sum[4][16];
+#pragma unroll
+        for (int q = 0; q < 4; ++q)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) sum[q][i] = 0.f;
+#pragma unroll 1
+        for (int kb = t.kb0; kb < t.kb1 && ok; kb += kLinSegment) {
           const int acc = local & 1;
           ok = wait_full(acc);
           if (!ok) break;
 #pragma unroll
-          for (int ch = 0; ch < 4; ++ch) {
-            uint32_t rr[32];
-            tc::tmem_ld_32x32(tmem_base + lanes + acc * 256 + half * 128 + ch * kLinChunk, rr);
+          for (int q = 0; q < 4; ++q) {
+            uint32_t rr[16];
+            tc::tmem_ld_32x16(tmem_base + lanes + acc * 256 + part * 64 + q * 16, rr);
             tc::tmem_ld_wait();
 #pragma unroll
-            for (int i = 0; i < 32; ++i) sum[ch][i] = first ? __uint_as_float(rr[i]) : sum[ch][i] + __uint_as_float(rr[i]);
+            for (int i = 0; i < 16; ++i) sum[q][i] += __uint_as_float(rr[i]);
           }
           release(acc);
         }
         if (!ok) break;
+        float* out = &p.dw[((int64_t)t.split * p.M + row0 + lane) * p.N + col0];
 #pragma unroll
-        for (int ch = 0; ch < 4; ++ch) {
-          if (ch >= nch) continue;
-          if (lane == 0) tc::bulk_wait_read<0>();
-          __syncwarp();
+        for (int ch = 0; ch < 2; ++ch) {
+          if (ch >= nch) continue;                        // (row0 < M: then all of the warp's rows are, M being a multiple of 64)
 #pragma unroll
-          for (int q = 0; q < 8; ++q)
-            *piece128(stg, lane, q) = make_uint4(__float_as_uint(sum[ch][4 * q]), __float_as_uint(sum[ch][4 * q + 1]),
-                                                 __float_as_uint(sum[ch][4 * q + 2]), __float_as_uint(sum[ch][4 * q + 3]));
-          tc::fence_proxy_async();
-          __syncwarp();
-          if (lane == 0) {
-            // (rows of the splits lie one after the other, M each: a tile that reaches beyond M ends at a warp's edge, M being
-            // a multiple of 64)
-            const int col = col0 + ch * kLinChunk, row = t.split * p.M + row0;
-            if (p.add) tc::tma_reduce_add_2d(&tmC, stg, col, row);
-            else tc::tma_store_2d(&tmC, stg, col, row);
-            tc::bulk_commit();
+          for (int q = 0; q < 4; ++q) {
+            float(&v)[16] = sum[2 * ch + q / 2];
+            float* o = out + ch * kLinChunk + 8 * q;
+            uint32_t w[8];
+            if (p.add) {
+              ld_sector(o, w, p.wide);
+#pragma unroll
+              for (int i = 0; i < 8; ++i) v[q % 2 * 8 + i] += __uint_as_float(w[i]);
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[q % 2 * 8 + i]);
+            st_sector(o, w, p.wide);
           }
         }
       } else {
         const int acc = local & 1;
-        auto ask = [&](int ch) {                          // lane 0: chunk ch of the residual into its staging tile
-          tc::bulk_wait_read<0>();                        // the store that last left from there
-          uint64_t* bar = &my_res[loaded & 1];
-          tc::mbar_expect_tx(bar, kLinBf16Chunk);
-          tc::tma_load_2d(stg + (loaded & 1) * kLinBf16Chunk, &tmR, bar, col0 + ch * kLinChunk, row0);
-        };
-        if (p.residual && nch > 0) {
-          if (lane == 0) ask(0);
-          ++loaded;
+        const bool mine = row0 + lane < p.M;
+        uint32_t r1[16];
+        if constexpr (kRes) {
+          if (lane == 0 && nch > 0) {
+            tc::bulk_wait_read<0>();                      // what last left from there
+            tc::mbar_expect_tx(&res_bar[ew], kLinTile);
+            tc::tma_load_2d(stg, &tmR, &res_bar[ew], col0, row0);
+          }
+          if (mine && nch > 1) {
+            const __nv_bfloat16* r = p.residual + ((int64_t)(row0 + lane) * p.N + col0 + kLinChunk);
+            ld_sector(r, r1, p.wide);
+            ld_sector(r + 16, r1 + 8, p.wide);
+          }
+          __syncwarp();
         }
         float xs = 1.f;
-        if (KIND == kLinFwd8 && row0 + lane < p.M) xs = __ldg(p.x_scale + row0 + lane);
+        if (KIND == kLinFwd8 && mine) xs = __ldg(p.x_scale + row0 + lane);
         ok = wait_full(acc);
         if (!ok) break;
-#pragma unroll 1
-        for (int ch = 0; ch < nch; ++ch, ++chunk) {
+#pragma unroll
+        for (int ch = 0; ch < 2; ++ch) {
+          if (ch >= nch) continue;
           const int col = col0 + ch * kLinChunk;
           uint32_t rr[32];
-          tc::tmem_ld_32x32(tmem_base + lanes + acc * 256 + half * 128 + ch * kLinChunk, rr);
-          if (p.residual && ch + 1 < nch) {
-            if (lane == 0) ask(ch + 1);
-            ++loaded;
-          }
+          Columns c;                                      // on their way while the accumulator is
+          tc::tmem_ld_32x32(tmem_base + lanes + acc * 256 + part * 64 + ch * kLinChunk, rr);
+          // (with a residual too there are no registers for that)
+          if (KIND == kLinFwd8 && !kRes) c.load(p.w_scale + col, p.vec);
+          if (KIND == kLinFwd && !kRes && p.bias != nullptr) c.load(p.bias + col, p.vec);
           tc::tmem_ld_wait();
+          if (ch + 1 == nch) release(acc);                // the accumulator is in registers
           float v[32];
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(rr[i]);
-          if constexpr (KIND == kLinFwd8) by_column(p.w_scale + col, p.vec, v, [&](float a, float s) { return a * (xs * s); });
-          uint8_t* buf = stg + (chunk & 1) * kLinBf16Chunk;
+          if constexpr (KIND == kLinFwd8) {
+            if (kRes) c.load(p.w_scale + col, p.vec);
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] *= xs * c.at(i);
+          }
+          if ((KIND == kLinFwd8 || (KIND == kLinFwd && kRes)) && p.bias != nullptr) c.load(p.bias + col, p.vec);
+          if (KIND != kLinDx && p.bias != nullptr) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] += c.at(i);
+          }
+          uint32_t r0[16];
+          auto take = [&] {                               // the first chunk's residual, out of the tile
+#pragma unroll
+            for (int q = 0; q < 4; ++q) {
+              const uint4 w = *piece(stg, lane, q);
+              r0[4 * q] = w.x; r0[4 * q + 1] = w.y; r0[4 * q + 2] = w.z; r0[4 * q + 3] = w.w;
+            }
+          };
+          if constexpr (kRes) {
+            if (ch == 0) {
+              ok = tc::mbar_wait_warp(&res_bar[ew], turn & 1, abort);
+              if (!ok) {
+                if (lane == 0) linear_timeout(p.status, abort, 45);
+                break;
+              }
+              ++turn;
+              if (kPre) take();
+            }
+          }
           if constexpr (KIND != kLinDx) {
-            if (p.bias != nullptr) by_column(p.bias + col, p.vec, v, [](float a, float b) { return a + b; });
-            if constexpr (kPre) {
-              if (lane == 1) tc::bulk_wait_read<1>();     // the store of two chunks ago
+            if (kPre || (!kRes && p.pre)) {               // leaves first, from the same tile
+              if ((!kRes || ch == 1) && lane == 0) tc::bulk_wait_read<0>();
               __syncwarp();
-              put_row(buf + 2 * kLinBf16Chunk, lane, v);
+              put_row(stg, lane, v);
+              tc::fence_proxy_async();
+              __syncwarp();
+              if (lane == 0) { tc::tma_store_2d(&tmP, stg, col, row0); tc::bulk_commit(); }
             }
             activate(v, p.act);
           }
-          if (p.residual) {
-            ok = tc::mbar_wait_warp(&my_res[chunk & 1], (chunk >> 1) & 1, abort);
-            if (!ok) {
-              if (lane == 0) linear_timeout(p.status, abort, 45);
-              break;
+          if constexpr (kRes) {
+            if (ch == 0 && !kPre) take();
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const uint32_t w = ch == 0 ? r0[i] : r1[i];
+              v[2 * i] += __uint_as_float(w << 16);
+              v[2 * i + 1] += __uint_as_float(w & 0xffff0000u);
             }
-            add_row(buf, lane, v);
-          } else {
-            if (lane == 0) tc::bulk_wait_read<1>();
-            __syncwarp();
           }
-          put_row(buf, lane, v);
+          if ((!kRes || kPre || ch == 1) && lane == 0) tc::bulk_wait_read<0>();
+          __syncwarp();
+          put_row(stg, lane, v);
           tc::fence_proxy_async();
           __syncwarp();
-          if (lane == 0) { tc::tma_store_2d(&tmC, buf, col, row0); tc::bulk_commit(); }
-          if (kPre && lane == 1) { tc::tma_store_2d(&tmP, buf + 2 * kLinBf16Chunk, col, row0); tc::bulk_commit(); }
+          if (lane == 0) { tc::tma_store_2d(&tmC, stg, col, row0); tc::bulk_commit(); }
         }
         if (!ok) break;
-        release(acc);
+        if (nch == 0) release(acc);
       }
     }
     if (!ok && lane == 0)
       for (int i = 0; i < 200; ++i) __nanosleep(1000);
-    if (lane < 2) tc::bulk_wait<0>();
+    if (lane == 0) tc::bulk_wait<0>();
     __syncwarp();
   }
 
@@ -375,16 +428,18 @@ LinearParams linear_params(const unipool_ctx* ctx, int M, int N, int kb_total, i
   return p;
 }
 
-template <int KIND, bool kPre>
+template <int KIND, bool kRes, bool kPre>
 int launch_linear(unipool_ctx* ctx, int phase, const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC,
                   const CUtensorMap& tmR, const CUtensorMap& tmP, const LinearParams& p, cudaStream_t s) {
   PhaseTimer pt(ctx, phase, 1, s);
-  auto kern = linear_pair_kernel<KIND, kPre>;
+  auto kern = linear_pair_kernel<KIND, kRes, kPre>;
   UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLinSmem));
   const int pairs = ctx->sm_count / 2;
   UP_KERNEL(kern, 2 * (p.units < pairs ? p.units : pairs), kLinThreads, kLinSmem, s, tmA, tmB, tmC, tmR, tmP, p);
   return UNIPOOL_OK;
 }
+
+template <typename... P> bool aligned(uintptr_t n, P... p) { return ((... | reinterpret_cast<uintptr_t>(p)) & (n - 1)) == 0; }
 
 #define UP_TRY(call)                     \
   do {                                   \
@@ -400,8 +455,8 @@ int linear_fwd_tc(unipool_ctx* ctx, const LinearArgs& a, cudaStream_t s) {
   LinearParams p = linear_params(ctx, a.T, a.n_out, (a.n_in + kb - 1) / kb, 1);
   p.act = a.act;
   p.bias = a.bias; p.x_scale = a.x_scale; p.w_scale = a.w_scale;
-  p.residual = a.residual != nullptr;
-  p.vec = ((reinterpret_cast<uintptr_t>(a.bias) | reinterpret_cast<uintptr_t>(a.w_scale)) & 15) == 0;
+  p.pre = a.pre != nullptr;
+  p.vec = aligned(16, a.bias, a.w_scale);
   CUtensorMap tmA, tmB, tmC, tmR, tmP;
   const MapKind kind = q8 ? kMapByteOperand : kMapOperand;
   UP_TRY(map_2d(ctx, &tmA, a.x, a.n_in, a.T, kb, 128, kind));
@@ -410,22 +465,26 @@ int linear_fwd_tc(unipool_ctx* ctx, const LinearArgs& a, cudaStream_t s) {
   tmR = tmP = tmC;
   if (a.residual != nullptr) UP_TRY(map_2d(ctx, &tmR, a.residual, a.n_out, a.T, kLinChunk, 32, kMapBf16Chunk));
   if (a.pre != nullptr) UP_TRY(map_2d(ctx, &tmP, a.pre, a.n_out, a.T, kLinChunk, 32, kMapBf16Chunk));
-  if (q8) return a.pre ? launch_linear<kLinFwd8, true>(ctx, UNIPOOL_PH_LINEAR, tmA, tmB, tmC, tmR, tmP, p, s)
-                       : launch_linear<kLinFwd8, false>(ctx, UNIPOOL_PH_LINEAR, tmA, tmB, tmC, tmR, tmP, p, s);
-  return a.pre ? launch_linear<kLinFwd, true>(ctx, UNIPOOL_PH_LINEAR, tmA, tmB, tmC, tmR, tmP, p, s)
-               : launch_linear<kLinFwd, false>(ctx, UNIPOOL_PH_LINEAR, tmA, tmB, tmC, tmR, tmP, p, s);
+  p.residual = static_cast<const __nv_bfloat16*>(a.residual);
+  p.wide = aligned(32, a.residual);
+  auto run = a.residual == nullptr ? (q8 ? launch_linear<kLinFwd8, false, false> : launch_linear<kLinFwd, false, false>)
+             : a.pre == nullptr    ? (q8 ? launch_linear<kLinFwd8, true, false> : launch_linear<kLinFwd, true, false>)
+                                   : (q8 ? launch_linear<kLinFwd8, true, true> : launch_linear<kLinFwd, true, true>);
+  return run(ctx, UNIPOOL_PH_LINEAR, tmA, tmB, tmC, tmR, tmP, p, s);
 }
 
 int linear_dx_tc(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, cudaStream_t s) {
   LinearParams p = linear_params(ctx, a.T, a.n_in, a.n_out / 64, 1);
-  p.residual = a.dx_residual != nullptr;
   CUtensorMap tmA, tmB, tmC, tmR;
   UP_TRY(map_2d(ctx, &tmA, dp, a.n_out, a.T, 64, 128));
   UP_TRY(map_mn(ctx, &tmB, a.W, a.n_in, a.n_out, 2));
   UP_TRY(map_2d(ctx, &tmC, a.dx, a.n_in, a.T, kLinChunk, 32, kMapBf16Chunk));
   tmR = tmC;
   if (a.dx_residual != nullptr) UP_TRY(map_2d(ctx, &tmR, a.dx_residual, a.n_in, a.T, kLinChunk, 32, kMapBf16Chunk));
-  return launch_linear<kLinDx, false>(ctx, UNIPOOL_PH_LINEAR_BWD, tmA, tmB, tmC, tmR, tmC, p, s);
+  p.residual = static_cast<const __nv_bfloat16*>(a.dx_residual);
+  p.wide = aligned(32, a.dx_residual);
+  auto run = a.dx_residual != nullptr ? launch_linear<kLinDx, true, false> : launch_linear<kLinDx, false, false>;
+  return run(ctx, UNIPOOL_PH_LINEAR_BWD, tmA, tmB, tmC, tmR, tmC, p, s);
 }
 
 // Parts of the tokens that the weight gradient is taken in, so that its tiles fill the CTA pairs: the number with the least
@@ -448,11 +507,12 @@ int linear_dw_splits_tc(const unipool_ctx* ctx, int T, int n_in, int n_out) {
 int linear_dw_tc(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, float* out, int splits, bool add, cudaStream_t s) {
   LinearParams p = linear_params(ctx, a.n_out, a.n_in, (a.T + 63) / 64, splits);
   p.add = add;
-  CUtensorMap tmA, tmB, tmC;
+  p.dw = out;
+  p.wide = aligned(32, out);
+  CUtensorMap tmA, tmB;
   UP_TRY(map_mn(ctx, &tmA, dp, a.n_out, a.T, 2));
   UP_TRY(map_mn(ctx, &tmB, a.x, a.n_in, a.T, 2));
-  UP_TRY(map_2d(ctx, &tmC, out, a.n_in, (uint64_t)splits * a.n_out, kLinChunk, 32, kMapF32Chunk));
-  return launch_linear<kLinDw, false>(ctx, UNIPOOL_PH_LINEAR_BWD, tmA, tmB, tmC, tmC, tmC, p, s);
+  return launch_linear<kLinDw, false, false>(ctx, UNIPOOL_PH_LINEAR_BWD, tmA, tmB, tmA, tmA, tmA, p, s);
 }
 
 }  // namespace unipool
