@@ -7,6 +7,7 @@
 #include "common.cuh"
 #include "linear_act.cuh"
 #include "simt_gemm.cuh"
+#include "vec.cuh"
 
 namespace unipool {
 
@@ -16,42 +17,7 @@ namespace {
 // dp = dy act'(p), rounded to the element type, and the column sums of the unrounded dp over the block's rows, into parts
 // [gridDim.y, N] (one row block: the gradient itself).  A thread owns V columns and every eighth row of the block's run;
 // eight rows' threads are added up in their order.  Bound by HBM (dy, p in, dp out).
-constexpr int kDpRows = 8;                               // rows a block has in hand at a time
-
-template <typename E, int V> struct Row;                 // V consecutive elements
-template <> struct Row<__nv_bfloat16, 8> {
-  static __device__ __forceinline__ void load(const __nv_bfloat16* p, float (&v)[8]) {
-    const uint4 r = __ldg(reinterpret_cast<const uint4*>(p));
-    const uint32_t w[4] = {r.x, r.y, r.z, r.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-  static __device__ __forceinline__ void store(__nv_bfloat16* p, const float (&v)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&b);
-    }
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-};
-template <> struct Row<float, 4> {
-  static __device__ __forceinline__ void load(const float* p, float (&v)[4]) {
-    const float4 r = __ldg(reinterpret_cast<const float4*>(p));
-    v[0] = r.x; v[1] = r.y; v[2] = r.z; v[3] = r.w;
-  }
-  static __device__ __forceinline__ void store(float* p, const float (&v)[4]) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  }
-};
-template <> struct Row<float, 1> {
-  static __device__ __forceinline__ void load(const float* p, float (&v)[1]) { v[0] = __ldg(p); }
-  static __device__ __forceinline__ void store(float* p, const float (&v)[1]) { *p = v[0]; }
-};
+constexpr int kDpRows = 8, kDpAhead = 4;                 // rows of a block's warps, rows that each has in flight
 
 struct DpParams {
   const void *dy, *p;
@@ -71,19 +37,29 @@ __global__ void __launch_bounds__(256) linear_dp_kernel(DpParams a) {
 #pragma unroll
   for (int j = 0; j < V; ++j) sum[j] = 0.f;
   if (c < a.N) {
-#pragma unroll 4
-    for (int t = t0 + g; t < t1; t += kDpRows) {
-      const int64_t at = (int64_t)t * a.N + c;
-      float d[V], p[V];
-      Row<E, V>::load(static_cast<const E*>(a.dy) + at, d);
-      if (a.dp != nullptr) {
-        Row<E, V>::load(static_cast<const E*>(a.p) + at, p);
+    for (int t = t0 + g; t < t1; t += kDpRows * kDpAhead) {
+      Vec<E, V> dy[kDpAhead], pre[kDpAhead];
 #pragma unroll
-        for (int j = 0; j < V; ++j) d[j] *= act_slope<kFast>(p[j], a.act);
-        Row<E, V>::store(static_cast<E*>(a.dp) + at, d);
+      for (int u = 0; u < kDpAhead; ++u) {
+        const int64_t at = (int64_t)(t + u * kDpRows) * a.N + c;
+        dy[u].zero();
+        if (t + u * kDpRows >= t1) continue;
+        dy[u].load(static_cast<const E*>(a.dy) + at);
+        if (a.dp != nullptr) pre[u].load(static_cast<const E*>(a.p) + at);
       }
 #pragma unroll
-      for (int j = 0; j < V; ++j) sum[j] += d[j];
+      for (int u = 0; u < kDpAhead; ++u) {
+        float d[V], p[V];
+        dy[u].get(d);
+        if (a.dp != nullptr && t + u * kDpRows < t1) {
+          pre[u].get(p);
+#pragma unroll
+          for (int j = 0; j < V; ++j) d[j] *= act_slope<kFast>(p[j], a.act);
+          Vec<E, V>::store(static_cast<E*>(a.dp) + (int64_t)(t + u * kDpRows) * a.N + c, d);
+        }
+#pragma unroll
+        for (int j = 0; j < V; ++j) sum[j] += d[j];
+      }
     }
   }
   if (a.parts == nullptr) return;
@@ -101,14 +77,15 @@ __global__ void __launch_bounds__(256) linear_dp_kernel(DpParams a) {
   }
 }
 
+// Rows of each of n row blocks: whole steps of the loop.
+int dp_rows(int T, int n) { return ((T + n - 1) / n + kDpRows * kDpAhead - 1) / (kDpRows * kDpAhead) * (kDpRows * kDpAhead); }
 // Row blocks of the kernel: so many that four blocks lie on an SM, of 32 rows at least.
 int dp_row_blocks(const unipool_ctx* ctx, int T, int N, int cols_per_block) {
   const int across = (N + cols_per_block - 1) / cols_per_block;
   int n = 4 * ctx->sm_count / across;
   if (n > (T + 31) / 32) n = (T + 31) / 32;
   if (n < 1) n = 1;
-  const int rows = (T + n - 1) / n;
-  return (T + rows - 1) / rows;
+  return (T + dp_rows(T, n) - 1) / dp_rows(T, n);
 }
 
 // ---------------------------------------------------------------- sums of parts, in their order
@@ -129,22 +106,25 @@ __global__ void __launch_bounds__(256) part_sum_kernel(const float* parts, int n
     out[c] = v.x; out[c + 1] = v.y; out[c + 2] = v.z; out[c + 3] = v.w;
   }
 }
-// Many parts of few columns: 32 columns to a block, its eight warps take every eighth part.
+// Many parts of few columns: eight columns, a sector, to a block, whose 32 groups of eight threads take every 32nd part.
 __global__ void __launch_bounds__(256) column_sum_kernel(const float* parts, int n_parts, int64_t width, float* out, bool add) {
   grid_wait(parts);
-  __shared__ float s[8][32];
-  const int g = threadIdx.x / 32;
-  const int64_t c = (int64_t)blockIdx.x * 32 + threadIdx.x % 32;
+  __shared__ float s[8][8];
+  const int lane = threadIdx.x % 32, g = threadIdx.x / 8;
+  const int64_t c = (int64_t)blockIdx.x * 8 + threadIdx.x % 8;
   float v = 0.f;
   if (c < width) {
 #pragma unroll 8
-    for (int i = g; i < n_parts; i += 8) v += __ldg(parts + i * width + c);
+    for (int i = g; i < n_parts; i += 32) v += __ldg(parts + i * width + c);
   }
-  s[g][threadIdx.x % 32] = v;
+  v += __shfl_xor_sync(0xffffffffu, v, 8);
+  v += __shfl_xor_sync(0xffffffffu, v, 16);
+  if (lane < 8) s[threadIdx.x / 32][lane] = v;
   __syncthreads();
-  if (g != 0 || c >= width) return;
+  if (threadIdx.x >= 8 || c >= width) return;
+  v = s[0][lane];
 #pragma unroll
-  for (int i = 1; i < 8; ++i) v += s[i][threadIdx.x];
+  for (int i = 1; i < 8; ++i) v += s[i][lane];
   out[c] = add ? out[c] + v : v;
 }
 
@@ -264,7 +244,7 @@ int dw_splits(const unipool_ctx* ctx, int T, int n_in, int n_out) {
 template <typename E, int V, bool kFast>
 int dp_as(unipool_ctx* ctx, const LinearBwdArgs& a, int* blocks, float* parts, cudaStream_t s) {
   const int n = dp_row_blocks(ctx, a.T, a.n_out, 32 * V);
-  DpParams p{a.dy, a.pre, a.act != UNIPOOL_ACT_NONE ? a.dp : nullptr, nullptr, a.T, a.n_out, (a.T + n - 1) / n, a.act, false};
+  DpParams p{a.dy, a.pre, a.act != UNIPOOL_ACT_NONE ? a.dp : nullptr, nullptr, a.T, a.n_out, dp_rows(a.T, n), a.act, false};
   if (a.dbias != nullptr) {
     p.parts = n > 1 ? parts : a.dbias;
     p.add = n == 1 && !a.overwrite;
@@ -282,7 +262,7 @@ int column_sum_launch(const float* parts, int n_parts, int64_t width, float* out
   if (width % 4 == 0 && width >= 4 * 256 * 148 && aligned16(parts))
     UP_KERNEL(part_sum_kernel, (unsigned)((width / 4 + 255) / 256), 256, 0, s, parts, n_parts, width, out, add);
   else
-    UP_KERNEL(column_sum_kernel, (unsigned)((width + 31) / 32), 256, 0, s, parts, n_parts, width, out, add);
+    UP_KERNEL(column_sum_kernel, (unsigned)((width + 7) / 8), 256, 0, s, parts, n_parts, width, out, add);
   return UNIPOOL_OK;
 }
 

@@ -2,6 +2,7 @@
 //   forward   y  = act(x W^T s_x s_w + bias) + residual   x, W K-major, bf16 or e4m3 with scales
 //   dx        dx = dp W (+ dx_residual)                   W MN-major
 //   dW        dW (+)= dp^T x                              both MN-major, fp32 out
+// Three forms: CTA pairs with tiles of 256 x 256 or 256 x 128, and a kernel for few tokens (below); the rule is linear_form.
 //
 // linear_pair_kernel: persistent CTA pairs as in the grouped kernels (expert_tc.cu): 256 x 256 tiles, M = 256 over both CTAs'
 // tensor memory, six 32 KB operand stages a CTA, accumulators double-buffered so that a tile's epilogue runs beside the next
@@ -11,6 +12,8 @@
 // the 3.1 us that they take.
 // Bound by the tensor pipe (operands through shared memory; see expert_tc.cu) and, held for long, by power.
 #include <cuda.h>
+
+#include <type_traits>
 
 #include "common.cuh"
 #include "linear_act.cuh"
@@ -24,7 +27,6 @@ namespace {
 enum LinearKind { kLinFwd, kLinFwd8, kLinDx, kLinDw };
 
 constexpr uint32_t kLinHalf = 128 * 128;                 // 128 rows (columns) x 128 bytes of one operand
-constexpr uint32_t kLinStage = 2 * kLinHalf;
 constexpr uint32_t kLinBars = 229376;                    // operand stages and staging tiles fill this much
 constexpr uint32_t kLinSmem = kLinBars + 512 + 1024;
 constexpr int kLinEpiWarps = 16;
@@ -130,15 +132,19 @@ __device__ __forceinline__ void activate(float (&v)[32], int act) {
 
 // kRes: a residual is added.  All of it is asked for before the accumulator is waited for: the first chunk's comes by TMA into
 // the staging tile, the second's into registers (a second tile for it would take an operand stage: 16384 tokens, 2048 -> 768 48.7
-// us instead of XX).  kPre: the value before the activation is stored too (one kernel with and without it where no residual is).
-template <int KIND, bool kRes, bool kPre>
+// us instead of 44.8).  kPre: the value before the activation is stored too (one kernel with and without it where no residual is).
+// kN: columns of a tile, 256 or 128.
+template <int KIND, int kN, bool kRes, bool kPre>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
 linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
                    const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmR,
                    const __grid_constant__ CUtensorMap tmP, LinearParams p) {
-  constexpr int kStages = KIND == kLinDw ? 7 : 6;
+  constexpr uint32_t kStage = kLinHalf + kN * 64;         // 128 rows of A, kN / 2 of B
+  constexpr int kStages = KIND == kLinDw ? 7 : kN == 256 ? 6 : 8;
   constexpr uint32_t kStaging = KIND == kLinDw ? 0 : kLinTile;
-  static_assert(kStages * kLinStage + kLinEpiWarps * kStaging == kLinBars, "shared memory");
+  static_assert(kStages * kStage + kLinEpiWarps * kStaging == kLinBars, "shared memory");
+  static_assert(kN == 256 || (kN == 128 && KIND != kLinDw), "columns of a tile");
+  constexpr int kPart = kN / 4, kChunks = kPart / kLinChunk;   // columns of an epilogue warp, its chunks
   constexpr bool kAMn = KIND == kLinDw, kBMn = KIND == kLinDx || KIND == kLinDw;
   constexpr int kKb = KIND == kLinFwd8 ? 128 : 64;       // elements of a k-block
   extern __shared__ uint8_t smem_raw[];
@@ -187,13 +193,13 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         const LinearUnit t = linear_unit(p, u);
         for (int kb = t.kb0; kb < t.kb1; ++kb) {
           if (!tc::mbar_wait(&empty_bar[stage], phase ^ 1u, abort)) { linear_timeout(p.status, abort, 41); ok = false; break; }
-          uint8_t* sA = smem + stage * kLinStage;
+          uint8_t* sA = smem + stage * kStage;
           uint8_t* sB = sA + kLinHalf;
-          if (rank == 0) tc::mbar_expect_tx(&full_bar[stage], 2 * kLinStage);      // both CTAs' bytes
+          if (rank == 0) tc::mbar_expect_tx(&full_bar[stage], 2 * kStage);         // both CTAs' bytes
           if constexpr (kAMn) tc::tma_load_3d_pair(sA, &tmA, &full_bar[stage], 0, kb * kKb, t.mt * 4 + rank * 2);
           else tc::tma_load_2d_pair(sA, &tmA, &full_bar[stage], kb * kKb, t.mt * 256 + rank * 128);
-          if constexpr (kBMn) tc::tma_load_3d_pair(sB, &tmB, &full_bar[stage], 0, kb * kKb, t.nt * 4 + rank * 2);
-          else tc::tma_load_2d_pair(sB, &tmB, &full_bar[stage], kb * kKb, t.nt * 256 + rank * 128);
+          if constexpr (kBMn) tc::tma_load_3d_pair(sB, &tmB, &full_bar[stage], 0, kb * kKb, (t.nt * 2 + rank) * (kN / 128));
+          else tc::tma_load_2d_pair(sB, &tmB, &full_bar[stage], kb * kKb, t.nt * kN + rank * (kN / 2));
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -203,7 +209,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer (leader CTA only)
     if (lane == 0 && rank == 0) {
-      constexpr uint32_t idesc = KIND == kLinFwd8 ? tc::instr_desc_e4m3(256, 256) : tc::instr_desc_bf16(256, kAMn, kBMn, 256);
+      constexpr uint32_t idesc = KIND == kLinFwd8 ? tc::instr_desc_e4m3(kN, 256) : tc::instr_desc_bf16(kN, kAMn, kBMn, 256);
       constexpr uint32_t a_lbo = kAMn ? kLinHalf / 2 : 16, b_lbo = kBMn ? kLinHalf / 2 : 16;
       constexpr uint32_t a_step = (kAMn ? 16 * 128 : 32) >> 4, b_step = (kBMn ? 16 * 128 : 32) >> 4;
       int stage = 0, local = 0;
@@ -222,7 +228,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
           for (; kb < end; ++kb) {
             if (!tc::mbar_wait(&full_bar[stage], phase, abort)) { linear_timeout(p.status, abort, 43); ok = false; break; }
             tc::tc_fence_after_sync();
-            const uint32_t a = tc::smem_u32(smem + stage * kLinStage);
+            const uint32_t a = tc::smem_u32(smem + stage * kStage);
             const uint64_t adesc = tc::smem_desc_sw128(a, a_lbo, 1024);
             const uint64_t bdesc = tc::smem_desc_sw128(a + kLinHalf, b_lbo, 1024);
 #pragma unroll
@@ -239,9 +245,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       }
     }
   } else {
-    // ------------------------------------------------------------ epilogue: 32 rows and 64 columns of the tile to a warp
+    // ------------------------------------------------------------ epilogue: 32 rows and a quarter of the tile's columns to a warp
     const int quarter = warp & 3, ew = warp - 2, part = ew >> 2;
-    uint8_t* stg = smem + kStages * kLinStage + ew * kStaging;
+    uint8_t* stg = smem + kStages * kStage + ew * kStaging;
     const uint32_t lanes = static_cast<uint32_t>(quarter * 32) << 16;
     int local = 0;
     uint32_t turn = 0;                                    // chunks of the residual that have landed in the staging tile
@@ -263,8 +269,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
     };
     for (int u = pair; u < p.units && ok; u += n_pairs) {
       const LinearUnit t = linear_unit(p, u);
-      const int row0 = t.mt * 256 + rank * 128 + quarter * 32, col0 = t.nt * 256 + part * 64;
-      const int nch = row0 < p.M ? max(0, min(2, (p.N - col0) / kLinChunk)) : 0;
+      const int row0 = t.mt * 256 + rank * 128 + quarter * 32, col0 = t.nt * kN + part * kPart;
+      const int nch = row0 < p.M ? max(0, min(kChunks, (p.N - col0) / kLinChunk)) : 0;
       if constexpr (KIND == kLinDw) {
         float sum[4][16];
 #pragma unroll
@@ -316,7 +322,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             tc::mbar_expect_tx(&res_bar[ew], kLinTile);
             tc::tma_load_2d(stg, &tmR, &res_bar[ew], col0, row0);
           }
-          if (mine && nch > 1) {
+          if (kChunks > 1 && mine && nch > 1) {
             const __nv_bfloat16* r = p.residual + ((int64_t)(row0 + lane) * p.N + col0 + kLinChunk);
             ld_sector(r, r1, p.wide);
             ld_sector(r + 16, r1 + 8, p.wide);
@@ -328,12 +334,12 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
         ok = wait_full(acc);
         if (!ok) break;
 #pragma unroll
-        for (int ch = 0; ch < 2; ++ch) {
+        for (int ch = 0; ch < kChunks; ++ch) {
           if (ch >= nch) continue;
           const int col = col0 + ch * kLinChunk;
           uint32_t rr[32];
           Columns c;                                      // on their way while the accumulator is
-          tc::tmem_ld_32x32(tmem_base + lanes + acc * 256 + part * 64 + ch * kLinChunk, rr);
+          tc::tmem_ld_32x32(tmem_base + lanes + acc * 256 + part * kPart + ch * kLinChunk, rr);
           // (with a residual too there are no registers for that)
           if (KIND == kLinFwd8 && !kRes) c.load(p.w_scale + col, p.vec);
           if (KIND == kLinFwd && !kRes && p.bias != nullptr) c.load(p.bias + col, p.vec);
@@ -417,10 +423,10 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   }
 }
 
-LinearParams linear_params(const unipool_ctx* ctx, int M, int N, int kb_total, int splits) {
+LinearParams linear_params(const unipool_ctx* ctx, int M, int N, int tile_n, int kb_total, int splits) {
   LinearParams p{};
   p.M = M; p.N = N;
-  p.n_mt = (M + 255) / 256; p.n_nt = (N + 255) / 256;
+  p.n_mt = (M + 255) / 256; p.n_nt = (N + tile_n - 1) / tile_n;
   p.kb_total = kb_total;
   p.kb_split = (kb_total + splits - 1) / splits;
   p.units = p.n_mt * p.n_nt * ((kb_total + p.kb_split - 1) / p.kb_split);
@@ -428,11 +434,11 @@ LinearParams linear_params(const unipool_ctx* ctx, int M, int N, int kb_total, i
   return p;
 }
 
-template <int KIND, bool kRes, bool kPre>
+template <int KIND, int kN, bool kRes, bool kPre>
 int launch_linear(unipool_ctx* ctx, int phase, const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC,
                   const CUtensorMap& tmR, const CUtensorMap& tmP, const LinearParams& p, cudaStream_t s) {
   PhaseTimer pt(ctx, phase, 1, s);
-  auto kern = linear_pair_kernel<KIND, kRes, kPre>;
+  auto kern = linear_pair_kernel<KIND, kN, kRes, kPre>;
   UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLinSmem));
   const int pairs = ctx->sm_count / 2;
   UP_KERNEL(kern, 2 * (p.units < pairs ? p.units : pairs), kLinThreads, kLinSmem, s, tmA, tmB, tmC, tmR, tmP, p);
@@ -447,44 +453,329 @@ template <typename... P> bool aligned(uintptr_t n, P... p) { return ((... | rein
     if (rc__ != UNIPOOL_OK) return rc__; \
   } while (0)
 
+// ---------------------------------------------------------------- few tokens
+// The weights on the M side: a CTA holds 128 features (A) against all of up to 128 tokens (N in steps of 16), S CTAs of a cluster
+// share a tile's contraction and add up through each other's shared memory, in the order of their ranks; each then finishes every
+// S-th token.  Bound by the weights' bytes and, below some megabytes of them, by latency: every CTA asks for all of its weights
+// at once as far as they fit its stages.
+constexpr int kFewTokens = 128, kFewMaxStages = 12, kFewThreads = 192;
+constexpr uint32_t kFewBars = 512;
+
+struct FewParams {
+  int T, M, N;                       // tokens of the call and of a tile (a multiple of 16); features of the result
+  int kb_total, stages, act;
+  const float *bias, *x_scale, *w_scale;
+  const __nv_bfloat16* residual;
+  __nv_bfloat16 *pre, *y;            // [T, M]
+  int32_t* status;
+};
+
+__device__ __forceinline__ float4 ld_cluster(uint32_t addr, uint32_t rank) {    // 16 bytes at `addr` of CTA `rank`
+  uint32_t remote;
+  float4 v;
+  asm volatile("mapa.shared::cluster.u32 %0, %1, %2;" : "=r"(remote) : "r"(addr), "r"(rank));
+  asm volatile("ld.shared::cluster.v4.f32 {%0, %1, %2, %3}, [%4];" : "=f"(v.x), "=f"(v.y), "=f"(v.z), "=f"(v.w) : "r"(remote) : "memory");
+  return v;
+}
+__device__ __forceinline__ void store_bf16x4(__nv_bfloat16* p, const float (&v)[4]) {
+  *reinterpret_cast<uint2*>(p) = make_uint2(tc::pack_bf16(v[0], v[1]), tc::pack_bf16(v[2], v[3]));
+}
+
+template <int KIND, int S>
+__global__ void __cluster_dims__(S, 1, 1) __launch_bounds__(kFewThreads)
+linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, FewParams p) {
+  constexpr bool kAMn = KIND == kLinDx;
+  constexpr int kKb = KIND == kLinFwd8 ? 128 : 64;
+  extern __shared__ uint8_t smem_raw[];
+  uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
+  uint64_t* full_bar = reinterpret_cast<uint64_t*>(smem);
+  uint64_t* empty_bar = full_bar + kFewMaxStages;
+  uint64_t* done_bar = empty_bar + kFewMaxStages;
+  uint32_t* tmem_ptr = reinterpret_cast<uint32_t*>(done_bar + 1);
+  volatile int* abort = reinterpret_cast<volatile int*>(tmem_ptr + 1);
+  static_assert((2 * kFewMaxStages + 1) * 8 + 8 <= kFewBars, "barrier block");
+  uint8_t* ring = smem + 1024;
+  float* sums = reinterpret_cast<float*>(ring);            // [N][128], once the products are complete
+  const uint32_t stage_bytes = kLinHalf + p.N * 128;
+
+  const int warp = threadIdx.x / 32, lane = threadIdx.x % 32;
+  const int rank = S > 1 ? (int)tc::cluster_ctarank() : 0;
+  const int m0 = blockIdx.x / S * 128, t0 = blockIdx.y * p.N;
+  const int kb0 = (int)((int64_t)p.kb_total * rank / S), n = (int)((int64_t)p.kb_total * (rank + 1) / S) - kb0;
+  if (threadIdx.x == 0) {
+    for (int s = 0; s < p.stages; ++s) { tc::mbar_init(&full_bar[s], 1); tc::mbar_init(&empty_bar[s], 1); }
+    tc::mbar_init(done_bar, 1);
+    *abort = 0;
+    tc::fence_barrier_init();
+    tc::tma_prefetch_desc(&tmW);
+    tc::tma_prefetch_desc(&tmX);
+  }
+  if (warp == 1) {
+    tc::tmem_alloc(tmem_ptr, 128);
+    tc::tmem_relinquish();
+  }
+  tc::tc_fence_before_sync();
+  __syncthreads();
+  tc::tc_fence_after_sync();
+  const uint32_t tmem = *tmem_ptr;
+  grid_wait(p.bias, p.x_scale, p.w_scale, p.residual);
+
+  if (warp == 0) {
+    if (lane == 0) {
+      int stage = 0;
+      uint32_t phase = 0;
+      bool ok = true;
+      for (int i = 0; i < n; ++i) {
+        ok = tc::mbar_wait(&empty_bar[stage], phase ^ 1u, abort);
+        if (!ok) { linear_timeout(p.status, abort, 51); break; }
+        uint8_t* sW = ring + stage * stage_bytes;
+        const int k = (kb0 + i) * kKb;
+        tc::mbar_expect_tx(&full_bar[stage], stage_bytes);
+        if constexpr (kAMn) tc::tma_load_3d(sW, &tmW, &full_bar[stage], 0, k, m0 / 64);
+        else tc::tma_load_2d(sW, &tmW, &full_bar[stage], k, m0);
+        tc::tma_load_2d(sW + kLinHalf, &tmX, &full_bar[stage], k, t0);
+        if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+      }
+      if (!ok)
+        for (int i = 0; i < 200; ++i) __nanosleep(1000);
+    }
+    __syncwarp();
+  } else if (warp == 1) {
+    if (lane == 0 && n > 0) {
+      const uint32_t idesc = KIND == kLinFwd8 ? tc::instr_desc_e4m3(p.N, 128) : tc::instr_desc_bf16(p.N, kAMn, false, 128);
+      constexpr uint32_t a_lbo = kAMn ? kLinHalf / 2 : 16, a_step = (kAMn ? 16 * 128 : 32) >> 4;
+      int stage = 0;
+      uint32_t phase = 0, accumulate = 0;
+      bool ok = true;
+      for (int i = 0; i < n; ++i) {
+        ok = tc::mbar_wait(&full_bar[stage], phase, abort);
+        if (!ok) { linear_timeout(p.status, abort, 52); break; }
+        tc::tc_fence_after_sync();
+        const uint32_t a = tc::smem_u32(ring + stage * stage_bytes);
+        const uint64_t adesc = tc::smem_desc_sw128(a, a_lbo, 1024), bdesc = tc::smem_desc_sw128(a + kLinHalf, 16, 1024);
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          if constexpr (KIND == kLinFwd8) tc::umma_e4m3(tmem, adesc + j * a_step, bdesc + j * 2, idesc, accumulate);
+          else tc::umma_bf16(tmem, adesc + j * a_step, bdesc + j * 2, idesc, accumulate);
+          accumulate = 1;
+        }
+        tc::umma_commit(&empty_bar[stage]);
+        if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+      }
+      if (ok) tc::umma_commit(done_bar);
+    }
+    __syncwarp();
+  } else {
+    const int quarter = warp & 3, f = quarter * 32 + lane;
+    bool some = n > 0;
+    if (some) {
+      some = tc::mbar_wait_warp(done_bar, 0, abort);
+      if (!some && lane == 0) linear_timeout(p.status, abort, 53);
+      tc::tc_fence_after_sync();
+    }
+    for (int c = 0; c < p.N; c += 16) {
+      uint32_t rr[16];
+      if (some) {
+        tc::tmem_ld_32x16(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + c, rr);
+        tc::tmem_ld_wait();
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) sums[(c + i) * 128 + f] = some ? __uint_as_float(rr[i]) : 0.f;
+    }
+    tc::tc_fence_before_sync();
+  }
+  if constexpr (S > 1) tc::cluster_sync(); else __syncthreads();   // every CTA's sums are there
+
+  // Four features to a lane, a token to a warp: of the cluster's 6 S warps each takes every 6 S-th token.
+  const int m = m0 + 4 * lane;
+  if (m < p.M) {
+    float4 b = make_float4(0.f, 0.f, 0.f, 0.f), ws = b;
+    if (KIND != kLinDx && p.bias != nullptr)
+      b = make_float4(__ldg(p.bias + m), __ldg(p.bias + m + 1), __ldg(p.bias + m + 2), __ldg(p.bias + m + 3));
+    if (KIND == kLinFwd8)
+      ws = make_float4(__ldg(p.w_scale + m), __ldg(p.w_scale + m + 1), __ldg(p.w_scale + m + 2), __ldg(p.w_scale + m + 3));
+    const uint32_t mine = tc::smem_u32(sums) + lane * 16;
+    constexpr int kWarps = kFewThreads / 32;
+#pragma unroll 2
+    for (int t = rank * kWarps + warp; t < p.N && t0 + t < p.T; t += S * kWarps) {
+      const int64_t at = (int64_t)(t0 + t) * p.M + m;
+      uint2 r = make_uint2(0u, 0u);
+      if (p.residual != nullptr) r = *reinterpret_cast<const uint2*>(&p.residual[at]);
+      const float xs = KIND == kLinFwd8 ? __ldg(p.x_scale + (t0 + t)) : 1.f;
+      float4 part[S];
+#pragma unroll
+      for (int q = 0; q < S; ++q) part[q] = S > 1 ? ld_cluster(mine + t * 512, q) : *reinterpret_cast<const float4*>(&sums[t * 128 + 4 * lane]);
+#pragma unroll
+      for (int q = 1; q < S; ++q) {
+        part[0].x += part[q].x; part[0].y += part[q].y; part[0].z += part[q].z; part[0].w += part[q].w;
+      }
+      float v[4] = {part[0].x, part[0].y, part[0].z, part[0].w};
+      if constexpr (KIND == kLinFwd8) { v[0] *= xs * ws.x; v[1] *= xs * ws.y; v[2] *= xs * ws.z; v[3] *= xs * ws.w; }
+      if constexpr (KIND != kLinDx) {
+        v[0] += b.x; v[1] += b.y; v[2] += b.z; v[3] += b.w;
+        if (p.pre != nullptr) store_bf16x4(&p.pre[at], v);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = act_value<true>(v[i], p.act);
+      }
+      v[0] += __uint_as_float(r.x << 16); v[1] += __uint_as_float(r.x & 0xffff0000u);
+      v[2] += __uint_as_float(r.y << 16); v[3] += __uint_as_float(r.y & 0xffff0000u);
+      store_bf16x4(&p.y[at], v);
+    }
+  }
+  if constexpr (S > 1) tc::cluster_sync(); else __syncthreads();   // no CTA leaves while another reads its sums
+  if (warp == 1) {
+    tc::tc_fence_after_sync();
+    tc::tmem_dealloc(tmem, 128);
+  }
+}
+
+template <int KIND, int S>
+int launch_few(unipool_ctx* ctx, int phase, const CUtensorMap& tmW, const CUtensorMap& tmX, const FewParams& p, uint32_t smem,
+               cudaStream_t s) {
+  PhaseTimer pt(ctx, phase, 1, s);
+  auto kern = linear_few_kernel<KIND, S>;
+  UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448));
+  UP_KERNEL(kern, dim3((p.M + 127) / 128 * S, (p.T + p.N - 1) / p.N), kFewThreads, smem, s, tmW, tmX, p);
+  return UNIPOOL_OK;
+}
+
+// How a call runs on the kernel for few tokens: a cluster of eight or four lies inside one GPC of 16 to 18 SMs, so that with two
+// CTAs on an SM 32 clusters of eight run at a time, 64 of four, 144 of two, and half as many with one (one more than that, and the
+// last come second: 384 tokens, 4096 -> 1536 on 36 clusters 19 us instead of 12).
+struct FewShape { int N, tiles, splits; bool half; };      // half: two CTAs share an SM's memory
+FewShape few_shape(int T, int M, int kb_total) {
+  FewShape f;
+  f.N = T < kFewTokens ? (T + 15) / 16 * 16 : kFewTokens;
+  f.tiles = (int)((int64_t)((M + 127) / 128) * ((T + f.N - 1) / f.N));
+  f.splits = f.tiles <= 28 ? 8 : f.tiles <= 60 ? 4 : f.tiles <= 140 ? 2 : 1;
+  while (f.splits > kb_total) f.splits /= 2;
+  f.half = f.tiles > (f.splits == 8 ? 16 : f.splits == 4 ? 32 : f.splits == 2 ? 72 : 148);
+  return f;
+}
+
+// Which kernel and which tile, by what they take for the call (us; M tokens, N features, k-blocks of 128 bytes).  The pairs: rounds of
+// tiles, 0.29 to 0.38 us a k-block (what shared memory moves; less while half the chip is idle), a start and an end.  The kernel
+// for few tokens: the bytes that its CTAs bring into an SM (85 a ns for one, 120 for two), and adding up.  Measured in us, few
+// tokens / 128 columns / 256 columns, bf16 with a residual:
+//   768 -> 2048   1 token 4.8/9.1/11.3    128 9.0/9.9/12.4    512 9.8/10.0/12.5    2048 14.4/15.5/13.3   8000 62.8/39.0/31.6
+//   4096 -> 1536  1 token 5.9/23.4/25.7   128 9.3/24.2/26.8   512 14.5/24.6/27.0   1501 30.7/27.0/27.7   8000 120/122/78
+//   4096 -> 128   1 token 6.0/23.2/24.5   512 8.9/24.2/25.0   8000 19.6/25.6/25.5
+//   128 -> 4096   1 token 4.9/8.8/11.7    512 9.9/7.3/9.8     8000 82.3/47.0/46.7
+enum LinearForm { kFew, kPairs128, kPairs256 };
+LinearForm linear_form(const unipool_ctx* ctx, int M, int N, int kb, bool plain) {
+  const int pairs = ctx->sm_count / 2;
+  auto by_pairs = [&](int n, double busy, double alone, double rest) {
+    const int64_t rounds = ((int64_t)((M + 255) / 256) * ((N + n - 1) / n) + pairs - 1) / pairs;
+    return (double)rounds * (kb * (rounds > 1 ? busy : alone) + 1.0) + rest;
+  };
+  const double p128 = by_pairs(128, 0.33, 0.30, plain ? 3.3 : 5.0), p256 = by_pairs(256, 0.38, 0.29, plain ? 4.1 : 8.0);
+  if (M <= 16 * 1024) {
+    const FewShape f = few_shape(M, N, kb);
+    const double ctas = (double)f.tiles * f.splits / ctx->sm_count, each = (kb + f.splits - 1) / f.splits * (16.0 + f.N / 8.0);
+    const double few = 3.2 + 0.03 * f.N + (ctas > 1.0 ? 0.7 + ctas * each / 120.0 : each / 85.0);
+    if (ctas <= 2.0 && few < p128 && few < p256) return kFew;     // (several rounds of its CTAs never were the fastest)
+  }
+  return p128 < p256 ? kPairs128 : kPairs256;
+}
+
+template <int KIND>
+int few_as(unipool_ctx* ctx, int phase, const CUtensorMap& tmW, const CUtensorMap& tmX, FewParams p, cudaStream_t s) {
+  const FewShape f = few_shape(p.T, p.M, p.kb_total);
+  const int splits = f.splits;
+  const uint32_t room = (f.half ? 113000u : 232448u) - 2048u, stage = kLinHalf + p.N * 128;
+  const int most = (int)(room / stage), need = (p.kb_total + splits - 1) / splits;
+  p.stages = most < kFewMaxStages ? most : kFewMaxStages;
+  if (p.stages > need) p.stages = need;
+  const uint32_t bytes = p.stages * stage > p.N * 512u ? p.stages * stage : p.N * 512u;   // the sums lie there too
+  auto run = splits == 8 ? launch_few<KIND, 8> : splits == 4 ? launch_few<KIND, 4> : splits == 2 ? launch_few<KIND, 2> : launch_few<KIND, 1>;
+  return run(ctx, phase, tmW, tmX, p, 2048 + bytes, s);
+}
+
 }  // namespace
+
+static int linear_few(unipool_ctx* ctx, const LinearArgs& a, cudaStream_t s) {
+  const bool q8 = a.x_scale != nullptr;
+  const int kb = q8 ? 128 : 64;
+  FewParams p{};
+  p.T = a.T; p.M = a.n_out;
+  p.kb_total = (a.n_in + kb - 1) / kb;
+  p.N = few_shape(p.T, p.M, p.kb_total).N;
+  p.act = a.act;
+  p.bias = a.bias; p.x_scale = a.x_scale; p.w_scale = a.w_scale;
+  p.residual = static_cast<const __nv_bfloat16*>(a.residual);
+  p.pre = static_cast<__nv_bfloat16*>(a.pre); p.y = static_cast<__nv_bfloat16*>(a.y);
+  p.status = ctx->ws.status;
+  CUtensorMap tmW, tmX;
+  const MapKind kind = q8 ? kMapByteOperand : kMapOperand;
+  UP_TRY(map_2d(ctx, &tmW, a.W, a.n_in, a.n_out, kb, 128, kind));
+  UP_TRY(map_2d(ctx, &tmX, a.x, a.n_in, a.T, kb, p.N, kind));
+  return q8 ? few_as<kLinFwd8>(ctx, UNIPOOL_PH_LINEAR, tmW, tmX, p, s) : few_as<kLinFwd>(ctx, UNIPOOL_PH_LINEAR, tmW, tmX, p, s);
+}
+
+static int linear_few_dx(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, cudaStream_t s) {
+  FewParams p{};
+  p.T = a.T; p.M = a.n_in;
+  p.kb_total = a.n_out / 64;
+  p.N = few_shape(p.T, p.M, p.kb_total).N;
+  p.residual = static_cast<const __nv_bfloat16*>(a.dx_residual);
+  p.y = static_cast<__nv_bfloat16*>(a.dx);
+  p.status = ctx->ws.status;
+  CUtensorMap tmW, tmX;
+  UP_TRY(map_mn(ctx, &tmW, a.W, a.n_in, a.n_out, 2));
+  UP_TRY(map_2d(ctx, &tmX, dp, a.n_out, a.T, 64, p.N));
+  return few_as<kLinDx>(ctx, UNIPOOL_PH_LINEAR_BWD, tmW, tmX, p, s);
+}
 
 int linear_fwd_tc(unipool_ctx* ctx, const LinearArgs& a, cudaStream_t s) {
   const bool q8 = a.x_scale != nullptr;
   const int kb = q8 ? 128 : 64;
-  LinearParams p = linear_params(ctx, a.T, a.n_out, (a.n_in + kb - 1) / kb, 1);
+  const LinearForm form = linear_form(ctx, a.T, a.n_out, (a.n_in + kb - 1) / kb, a.bias == nullptr && a.act == UNIPOOL_ACT_NONE);
+  if (form == kFew) return linear_few(ctx, a, s);
+  const int tile_n = form == kPairs128 ? 128 : 256;
+  LinearParams p = linear_params(ctx, a.T, a.n_out, tile_n, (a.n_in + kb - 1) / kb, 1);
   p.act = a.act;
   p.bias = a.bias; p.x_scale = a.x_scale; p.w_scale = a.w_scale;
   p.pre = a.pre != nullptr;
   p.vec = aligned(16, a.bias, a.w_scale);
+  p.residual = static_cast<const __nv_bfloat16*>(a.residual);
+  p.wide = aligned(32, a.residual);
   CUtensorMap tmA, tmB, tmC, tmR, tmP;
   const MapKind kind = q8 ? kMapByteOperand : kMapOperand;
   UP_TRY(map_2d(ctx, &tmA, a.x, a.n_in, a.T, kb, 128, kind));
-  UP_TRY(map_2d(ctx, &tmB, a.W, a.n_in, a.n_out, kb, 128, kind));
+  UP_TRY(map_2d(ctx, &tmB, a.W, a.n_in, a.n_out, kb, tile_n / 2, kind));
   UP_TRY(map_2d(ctx, &tmC, a.y, a.n_out, a.T, kLinChunk, 32, kMapBf16Chunk));
   tmR = tmP = tmC;
   if (a.residual != nullptr) UP_TRY(map_2d(ctx, &tmR, a.residual, a.n_out, a.T, kLinChunk, 32, kMapBf16Chunk));
   if (a.pre != nullptr) UP_TRY(map_2d(ctx, &tmP, a.pre, a.n_out, a.T, kLinChunk, 32, kMapBf16Chunk));
-  p.residual = static_cast<const __nv_bfloat16*>(a.residual);
-  p.wide = aligned(32, a.residual);
-  auto run = a.residual == nullptr ? (q8 ? launch_linear<kLinFwd8, false, false> : launch_linear<kLinFwd, false, false>)
-             : a.pre == nullptr    ? (q8 ? launch_linear<kLinFwd8, true, false> : launch_linear<kLinFwd, true, false>)
-                                   : (q8 ? launch_linear<kLinFwd8, true, true> : launch_linear<kLinFwd, true, true>);
-  return run(ctx, UNIPOOL_PH_LINEAR, tmA, tmB, tmC, tmR, tmP, p, s);
+  auto as = [&](auto n) {
+    constexpr int N = decltype(n)::value;
+    auto run = a.residual == nullptr ? (q8 ? launch_linear<kLinFwd8, N, false, false> : launch_linear<kLinFwd, N, false, false>)
+               : a.pre == nullptr    ? (q8 ? launch_linear<kLinFwd8, N, true, false> : launch_linear<kLinFwd, N, true, false>)
+                                     : (q8 ? launch_linear<kLinFwd8, N, true, true> : launch_linear<kLinFwd, N, true, true>);
+    return run(ctx, UNIPOOL_PH_LINEAR, tmA, tmB, tmC, tmR, tmP, p, s);
+  };
+  return tile_n == 256 ? as(std::integral_constant<int, 256>()) : as(std::integral_constant<int, 128>());
 }
 
 int linear_dx_tc(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, cudaStream_t s) {
-  LinearParams p = linear_params(ctx, a.T, a.n_in, a.n_out / 64, 1);
+  const LinearForm form = linear_form(ctx, a.T, a.n_in, a.n_out / 64, true);
+  if (form == kFew) return linear_few_dx(ctx, a, dp, s);
+  const int tile_n = form == kPairs128 ? 128 : 256;
+  LinearParams p = linear_params(ctx, a.T, a.n_in, tile_n, a.n_out / 64, 1);
+  p.residual = static_cast<const __nv_bfloat16*>(a.dx_residual);
+  p.wide = aligned(32, a.dx_residual);
   CUtensorMap tmA, tmB, tmC, tmR;
   UP_TRY(map_2d(ctx, &tmA, dp, a.n_out, a.T, 64, 128));
-  UP_TRY(map_mn(ctx, &tmB, a.W, a.n_in, a.n_out, 2));
+  UP_TRY(map_mn(ctx, &tmB, a.W, a.n_in, a.n_out, tile_n / 128));
   UP_TRY(map_2d(ctx, &tmC, a.dx, a.n_in, a.T, kLinChunk, 32, kMapBf16Chunk));
   tmR = tmC;
   if (a.dx_residual != nullptr) UP_TRY(map_2d(ctx, &tmR, a.dx_residual, a.n_in, a.T, kLinChunk, 32, kMapBf16Chunk));
-  p.residual = static_cast<const __nv_bfloat16*>(a.dx_residual);
-  p.wide = aligned(32, a.dx_residual);
-  auto run = a.dx_residual != nullptr ? launch_linear<kLinDx, true, false> : launch_linear<kLinDx, false, false>;
-  return run(ctx, UNIPOOL_PH_LINEAR_BWD, tmA, tmB, tmC, tmR, tmC, p, s);
+  auto as = [&](auto n) {
+    constexpr int N = decltype(n)::value;
+    auto run = a.dx_residual != nullptr ? launch_linear<kLinDx, N, true, false> : launch_linear<kLinDx, N, false, false>;
+    return run(ctx, UNIPOOL_PH_LINEAR_BWD, tmA, tmB, tmC, tmR, tmC, p, s);
+  };
+  return tile_n == 256 ? as(std::integral_constant<int, 256>()) : as(std::integral_constant<int, 128>());
 }
 
 // Parts of the tokens that the weight gradient is taken in, so that its tiles fill the CTA pairs: the number with the least
@@ -505,14 +796,14 @@ int linear_dw_splits_tc(const unipool_ctx* ctx, int T, int n_in, int n_out) {
 
 // out [splits, n_out, n_in]: the parts' sums, or with one part the gradient.
 int linear_dw_tc(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, float* out, int splits, bool add, cudaStream_t s) {
-  LinearParams p = linear_params(ctx, a.n_out, a.n_in, (a.T + 63) / 64, splits);
+  LinearParams p = linear_params(ctx, a.n_out, a.n_in, 256, (a.T + 63) / 64, splits);
   p.add = add;
   p.dw = out;
   p.wide = aligned(32, out);
   CUtensorMap tmA, tmB;
   UP_TRY(map_mn(ctx, &tmA, dp, a.n_out, a.T, 2));
   UP_TRY(map_mn(ctx, &tmB, a.x, a.n_in, a.T, 2));
-  return launch_linear<kLinDw, false, false>(ctx, UNIPOOL_PH_LINEAR_BWD, tmA, tmB, tmA, tmA, tmA, p, s);
+  return launch_linear<kLinDw, 256, false, false>(ctx, UNIPOOL_PH_LINEAR_BWD, tmA, tmB, tmA, tmA, tmA, p, s);
 }
 
 }  // namespace unipool

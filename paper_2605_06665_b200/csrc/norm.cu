@@ -14,6 +14,8 @@
 #include <type_traits>
 
 #include "common.cuh"
+#include "tc_ptx.cuh"
+#include "vec.cuh"
 
 namespace unipool {
 
@@ -23,50 +25,12 @@ constexpr int kNormMaxWidth = 16384;
 constexpr float kE4m3Max = 448.f;
 constexpr float kSmallestScale = 1.17549435e-38f;        // 2^-126: its reciprocal is finite, a row of zeros keeps zeros
 
-// V consecutive elements as they lie in memory: 16 bytes, or a single element where those do not fit.
-template <typename E, int V> struct Vec;
-template <> struct Vec<__nv_bfloat16, 8> {
-  uint4 raw;
-  __device__ __forceinline__ void load(const __nv_bfloat16* p) { raw = *reinterpret_cast<const uint4*>(p); }
-  __device__ __forceinline__ void zero() { raw = make_uint4(0, 0, 0, 0); }
-  __device__ __forceinline__ void get(float (&v)[8]) const {
-    const uint32_t w[4] = {raw.x, raw.y, raw.z, raw.w};
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      v[2 * i] = __uint_as_float(w[i] << 16);
-      v[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
-    }
-  }
-  __device__ __forceinline__ static void store(__nv_bfloat16* p, const float (&v)[8]) {
-    uint32_t w[4];
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const __nv_bfloat162 b = __floats2bfloat162_rn(v[2 * i], v[2 * i + 1]);
-      w[i] = *reinterpret_cast<const uint32_t*>(&b);
-    }
-    *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
-  }
-};
-template <> struct Vec<float, 4> {
-  float4 raw;
-  __device__ __forceinline__ void load(const float* p) { raw = *reinterpret_cast<const float4*>(p); }
-  __device__ __forceinline__ void zero() { raw = make_float4(0.f, 0.f, 0.f, 0.f); }
-  __device__ __forceinline__ void get(float (&v)[4]) const { v[0] = raw.x; v[1] = raw.y; v[2] = raw.z; v[3] = raw.w; }
-  __device__ __forceinline__ static void store(float* p, const float (&v)[4]) {
-    *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
-  }
-};
-template <typename E> struct Vec<E, 1> {
-  E raw;
-  __device__ __forceinline__ void load(const E* p) { raw = *p; }
-  __device__ __forceinline__ void zero() { raw = from_f32<E>(0.f); }
-  __device__ __forceinline__ void get(float (&v)[1]) const { v[0] = to_f32(raw); }
-  __device__ __forceinline__ static void store(E* p, const float (&v)[1]) { *p = from_f32<E>(v[0]); }
-};
-
 template <int V> __device__ __forceinline__ void load_w(const float* w, float (&v)[V]) {
   if constexpr (V == 1) {
     v[0] = __ldg(w);
+  } else if constexpr (V == 2) {
+    const float2 f = __ldg(reinterpret_cast<const float2*>(w));
+    v[0] = f.x; v[1] = f.y;
   } else {
 #pragma unroll
     for (int i = 0; i < V; i += 4) {
@@ -201,109 +165,280 @@ struct NormBwdParams {
   const float *w, *rstd;
   void* dx;
   float* dw;        // [blocks, width] sums of the blocks; one block: the gradient itself
-  int T, width;
+  int T, width, stages;
   bool add;         // one block: add to what dw holds
+  int32_t* status;
 };
 
-template <int TPR> constexpr int kNormBwdThreads = TPR == 32 ? 256 : TPR;
+// The sums over the warp of each of R values: the lane's own value of row row_of_lane<R>(lane) on return.  A lane hands half of its
+// values over at each step, until it has one.
+template <int R> __device__ __forceinline__ float reduce_rows(float (&v)[R], int lane) {
+  static_assert(R == 1 || R == 2 || R == 4 || R == 8, "rows");
+  if constexpr (R == 8) {
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const float give = lane & 16 ? v[k] : v[k + 4];
+      v[k] = (lane & 16 ? v[k + 4] : v[k]) + __shfl_xor_sync(0xffffffffu, give, 16);
+    }
+  }
+  if constexpr (R >= 4) {
+    constexpr int o = R == 8 ? 8 : 16;
+#pragma unroll
+    for (int k = 0; k < 2; ++k) {
+      const float give = lane & o ? v[k] : v[k + 2];
+      v[k] = (lane & o ? v[k + 2] : v[k]) + __shfl_xor_sync(0xffffffffu, give, o);
+    }
+  }
+  if constexpr (R >= 2) {
+    constexpr int o = 32 / R;
+    const float give = lane & o ? v[0] : v[1];
+    v[0] = (lane & o ? v[1] : v[0]) + __shfl_xor_sync(0xffffffffu, give, o);
+  }
+#pragma unroll
+  for (int o = 16 / R; o > 0; o >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], o);
+  return v[0];
+}
+template <int R> __device__ __forceinline__ int row_of_lane(int lane) { return lane / (32 / R); }
 
-// Blocks walk over the rows; a thread sums dw of its columns over its rows, a block over its warps in their order, so that the
-// result does not depend on who is first.
-template <typename E, int V, int TPR, int VPT>
-__global__ void __launch_bounds__(kNormBwdThreads<TPR>) rmsnorm_bwd_kernel(NormBwdParams p) {
+// A block takes R rows at a time and a thread VPT vectors of the same columns of each: it keeps w and its sums for dw in
+// registers over all its rows, and the rows' dot products cost one barrier for R of them.  (With a row to a warp the sums of a whole
+// row lay in every warp's registers, and they had to be added up at the end: 16384 rows of 768 bf16 22.5 us instead of 19.5, and more to add up behind it.)
+// kRing: R rows are one run of bytes in memory, a multiple of 16 of them; runs are copied into a ring in shared memory some
+// stages ahead, so that reads go on while rows are worked on and whatever the rows' alignment (16384 rows of 770 bf16 read
+// element by element 69 us, through the ring 37).  Without it (arrays off 16 bytes, rows too long for two stages) the loads go
+// from memory into registers.
+// The sums' order depends on the sizes alone.
+template <typename E, int V, int VPT, int R, bool kRing>
+__global__ void __launch_bounds__(512) rmsnorm_bwd_kernel(NormBwdParams p) {
+  extern __shared__ __align__(128) uint8_t ring[];       // [stages][dh, r, dr][R rows], then the barriers
+  __shared__ float part[2][16][R];
+  __shared__ int abort_word;
+  constexpr bool kKeepW = VPT * V <= 16;                 // else w comes from the cache again
+  const int t = threadIdx.x, n_warps = blockDim.x / 32;
+  const uint32_t run = (uint32_t)(R * p.width * (int)sizeof(E));
+  const int arrays = p.dr != nullptr ? 3 : 2;
+  uint64_t* full = reinterpret_cast<uint64_t*>(ring + (size_t)p.stages * arrays * run);
+  volatile int* abort = &abort_word;
+  if constexpr (kRing) {
+    if (t == 0) {
+      for (int s = 0; s < p.stages; ++s) tc::mbar_init(&full[s], 1);
+      *abort = 0;
+      tc::fence_barrier_init();
+    }
+    __syncthreads();
+  }
   grid_wait(p.dh, p.r, p.dr, p.w, p.rstd);
-  extern __shared__ float sums[];                        // [width] (TPR = 32)
-  __shared__ float part[2][TPR > 32 ? TPR / 32 : 1];
-  constexpr int kRows = kNormBwdThreads<TPR> / TPR;
-  const int t = threadIdx.x % TPR;
-  float dw[VPT][V];
+  const int64_t groups = ((int64_t)p.T + R - 1) / R;
+  // Rows of group g into its stage: by the copy engine, if they end on 16 bytes (the last ones may not).
+  auto bytes_of = [&](int64_t g) { return (uint32_t)(min((int64_t)R, p.T - g * R) * p.width * (int)sizeof(E)); };
+  auto fetch = [&](int64_t g, int stage) {
+    const uint32_t n = bytes_of(g);
+    if (n % 16 != 0) return;
+    uint8_t* to = ring + (size_t)stage * arrays * run;
+    const int64_t from = g * run;
+    tc::mbar_expect_tx(&full[stage], arrays * n);
+    tc::bulk_load(to, static_cast<const uint8_t*>(p.dh) + from, n, &full[stage]);
+    tc::bulk_load(to + run, static_cast<const uint8_t*>(p.r) + from, n, &full[stage]);
+    if (arrays == 3) tc::bulk_load(to + 2 * run, static_cast<const uint8_t*>(p.dr) + from, n, &full[stage]);
+  };
+  if (kRing && t == 0) {
+    int64_t g = blockIdx.x;
+    for (int s = 0; s < p.stages && g < groups; ++s, g += gridDim.x) fetch(g, s);
+  }
+  auto column = [&](int i) { return (i * (int)blockDim.x + t) * V; };
+  float dw[VPT][V], w[kKeepW ? VPT : 1][V];
 #pragma unroll
   for (int i = 0; i < VPT; ++i)
 #pragma unroll
     for (int j = 0; j < V; ++j) dw[i][j] = 0.f;
-  int turn = 0;
-  for (int64_t row = blockIdx.x * kRows + threadIdx.x / TPR; row < p.T; row += (int64_t)gridDim.x * kRows, turn ^= 1) {
-    const int64_t at = row * p.width;
-    const E* dh = static_cast<const E*>(p.dh) + at;
-    const E* r = static_cast<const E*>(p.r) + at;
-    const E* dr = static_cast<const E*>(p.dr) + at;
-    Vec<E, V> a[VPT], b[VPT], d[VPT];
+  if constexpr (kKeepW) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const int c = (i * TPR + t) * V;
-      a[i].zero();
-      b[i].zero();
-      if (c < p.width) { a[i].load(dh + c); b[i].load(r + c); }
+    for (int i = 0; i < VPT; ++i)
+      if (column(i) < p.width) load_w<V>(p.w + column(i), w[i]);
+  }
+  const float inv_width = 1.f / (float)p.width;
+  int turn = 0, stage = 0;
+  uint32_t phase = 0;
+  float n_next[R];                                       // rstd of the next rows
+  auto load_rstd = [&](int64_t g) {
+#pragma unroll
+    for (int k = 0; k < R; ++k) n_next[k] = g * R + k < p.T ? __ldg(p.rstd + (g * R + k)) : 0.f;
+  };
+  load_rstd(blockIdx.x);
+  for (int64_t g = blockIdx.x; g < groups; g += gridDim.x, turn ^= 1) {
+    const int64_t row0 = g * R;
+    const uint8_t* at_stage = ring + (size_t)stage * arrays * run;
+    if constexpr (kRing) {
+      if (bytes_of(g) % 16 == 0) {
+        // (a wait that runs out is reported, and no later one waits; the block goes on to its end)
+        if (!*abort && !tc::mbar_wait(&full[stage], phase, abort)) {
+          *abort = 1;
+          if (atomicCAS(p.status, 0, kStatusTimeout) == 0) { p.status[1] = 61; p.status[2] = (int)blockIdx.x; }
+        }
+      } else {
+        const int64_t from = row0 * p.width;
+        for (int c = t; c < (int)(p.T - row0) * p.width; c += blockDim.x) {
+          E* to = reinterpret_cast<E*>(ring + (size_t)stage * arrays * run) + c;
+          to[0] = static_cast<const E*>(p.dh)[from + c];
+          to[R * p.width] = static_cast<const E*>(p.r)[from + c];
+          if (arrays == 3) to[2 * R * p.width] = static_cast<const E*>(p.dr)[from + c];
+        }
+        __syncthreads();
+      }
     }
-    if (p.dr != nullptr) {
+    Vec<E, V> a[R][VPT], b[R][VPT], d[R][VPT];
+    float n[R], dot[R];
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      const bool live = row0 + k < p.T;
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
-        const int c = (i * TPR + t) * V;
-        d[i].zero();
-        if (c < p.width) d[i].load(dr + c);
-      }
-    }
-    const float n = __ldg(p.rstd + row);
-    float dot = 0.f;
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const int c = (i * TPR + t) * V;
-      if (c >= p.width) continue;
-      float u[V], v[V], w[V];
-      a[i].get(u);
-      b[i].get(v);
-      load_w<V>(p.w + c, w);
-#pragma unroll
-      for (int j = 0; j < V; ++j) {
-        dw[i][j] = fmaf(u[j], v[j] * n, dw[i][j]);
-        dot = fmaf(u[j] * w[j], v[j], dot);
-      }
-    }
-    dot = row_reduce<TPR>(dot, part[turn], [](float m, float o) { return m + o; });   // (two, for the next row's writers)
-    const float k = n * n * n * (dot / (float)p.width);
-#pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const int c = (i * TPR + t) * V;
-      if (c >= p.width) continue;
-      float u[V], v[V], w[V];
-      a[i].get(u);
-      b[i].get(v);
-      load_w<V>(p.w + c, w);
-#pragma unroll
-      for (int j = 0; j < V; ++j) u[j] = n * w[j] * u[j] - v[j] * k;
-      if (p.dr != nullptr) {
-        d[i].get(v);
-#pragma unroll
-        for (int j = 0; j < V; ++j) u[j] += v[j];
-      }
-      Vec<E, V>::store(static_cast<E*>(p.dx) + at + c, u);
-    }
-  }
-  if (p.dw == nullptr) return;
-  float* out = &p.dw[(int64_t)blockIdx.x * p.width];
-  if constexpr (TPR == 32) {
-    for (int g = 0; g < kRows; ++g) {
-      if ((int)threadIdx.x / 32 == g) {
-#pragma unroll
-        for (int i = 0; i < VPT; ++i) {
-          const int c = (i * TPR + t) * V;
-          if (c >= p.width) continue;
-#pragma unroll
-          for (int j = 0; j < V; ++j) sums[c + j] = g == 0 ? dw[i][j] : sums[c + j] + dw[i][j];
+        const int c = column(i);
+        a[k][i].zero();
+        b[k][i].zero();
+        if (live && c < p.width) {
+          const E *x, *y, *z;
+          if constexpr (kRing) {
+            x = reinterpret_cast<const E*>(at_stage) + (k * p.width + c);
+            y = x + R * p.width;
+            z = y + R * p.width;
+          } else {
+            const int64_t at = (row0 + k) * p.width + c;
+            x = static_cast<const E*>(p.dh) + at;
+            y = static_cast<const E*>(p.r) + at;
+            z = static_cast<const E*>(p.dr) + at;
+          }
+          a[k][i].load(x);
+          b[k][i].load(y);
+          if (p.dr != nullptr) d[k][i].load(z);
         }
       }
-      __syncthreads();
+      n[k] = n_next[k];
     }
-    for (int c = threadIdx.x; c < p.width; c += blockDim.x) out[c] = p.add ? out[c] + sums[c] : sums[c];
-  } else {
+    load_rstd(g + gridDim.x);
 #pragma unroll
-    for (int i = 0; i < VPT; ++i) {
-      const int c = (i * TPR + t) * V;
-      if (c >= p.width) continue;
+    for (int k = 0; k < R; ++k) {
+      dot[k] = 0.f;
 #pragma unroll
-      for (int j = 0; j < V; ++j) out[c + j] = p.add ? out[c + j] + dw[i][j] : dw[i][j];
+      for (int i = 0; i < VPT; ++i) {
+        const int c = column(i);
+        if (c >= p.width) continue;
+        float u[V], v[V];
+        a[k][i].get(u);
+        b[k][i].get(v);
+        float(&wi)[V] = w[kKeepW ? i : 0];
+        if (!kKeepW) load_w<V>(p.w + c, wi);
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+          dw[i][j] = fmaf(u[j], v[j] * n[k], dw[i][j]);
+          dot[k] = fmaf(u[j] * wi[j], v[j], dot[k]);
+        }
+      }
+    }
+    {
+      const float sum = reduce_rows<R>(dot, t % 32);
+      if (t % (32 / R) == 0) part[turn][t / 32][row_of_lane<R>(t % 32)] = sum;
+    }
+    __syncthreads();                                     // (two arrays in turn: the next rows' sums need no second barrier)
+    if constexpr (kRing) {                               // the stage is in registers: on to the rows that lie `stages` further
+      if (t == 0 && g + (int64_t)p.stages * gridDim.x < groups && !*abort) fetch(g + (int64_t)p.stages * gridDim.x, stage);
+      if (++stage == p.stages) { stage = 0; phase ^= 1u; }
+    }
+    if (n_warps <= 4) {
+#pragma unroll
+      for (int k = 0; k < R; ++k) dot[k] = part[turn][0][k];
+      for (int q = 1; q < n_warps; ++q)
+#pragma unroll
+        for (int k = 0; k < R; ++k) dot[k] += part[turn][q][k];
+    } else {                                             // a warp's sum to a lane, half of the rows to either half of the lanes
+      constexpr int H = R > 1 ? R / 2 : 1;
+      const int q = t % 16, first = R > 1 ? (t / 16 % 2) * H : 0;
+      float half[H];
+#pragma unroll
+      for (int k = 0; k < H; ++k) half[k] = q < n_warps ? part[turn][q][first + k] : 0.f;
+#pragma unroll
+      for (int o = 8; o > 0; o >>= 1)
+#pragma unroll
+        for (int k = 0; k < H; ++k) half[k] += __shfl_xor_sync(0xffffffffu, half[k], o);
+#pragma unroll
+      for (int k = 0; k < H; ++k) {
+        const float other = __shfl_xor_sync(0xffffffffu, half[k], 16);
+        dot[k] = first == 0 ? half[k] : other;
+        if constexpr (R > 1) dot[H + k] = first == 0 ? other : half[k];
+      }
+    }
+#pragma unroll
+    for (int k = 0; k < R; ++k) {
+      if (row0 + k >= p.T) break;
+      const float s = n[k] * n[k] * n[k] * (dot[k] * inv_width);
+#pragma unroll
+      for (int i = 0; i < VPT; ++i) {
+        const int c = column(i);
+        if (c >= p.width) continue;
+        float u[V], v[V];
+        a[k][i].get(u);
+        b[k][i].get(v);
+        float(&wi)[V] = w[kKeepW ? i : 0];
+        if (!kKeepW) load_w<V>(p.w + c, wi);
+#pragma unroll
+        for (int j = 0; j < V; ++j) u[j] = n[k] * wi[j] * u[j] - v[j] * s;
+        if (p.dr != nullptr) {
+          d[k][i].get(v);
+#pragma unroll
+          for (int j = 0; j < V; ++j) u[j] += v[j];
+        }
+        Vec<E, V>::store(static_cast<E*>(p.dx) + (row0 + k) * p.width + c, u);
+      }
     }
   }
+  if (kRing && *abort)
+    for (int i = 0; i < 200; ++i) __nanosleep(1000);     // let copies already in flight land before the block retires
+  if (p.dw == nullptr) return;
+  float* out = &p.dw[(int64_t)blockIdx.x * p.width];
+#pragma unroll
+  for (int i = 0; i < VPT; ++i) {
+    const int c = column(i);
+    if (c >= p.width) continue;
+#pragma unroll
+    for (int j = 0; j < V; ++j) out[c + j] = p.add ? out[c + j] + dw[i][j] : dw[i][j];
+  }
+}
+
+// How the backward kernel runs: elements of a vector, vectors of a thread, threads and rows of a block, blocks, stages of the ring
+// (0: none) and its bytes.
+struct NormBwdShape { int v, vpt, threads, rows, blocks, stages; uint32_t smem; };
+constexpr int norm_bwd_rows(int V, int bytes, int vpt) {   // 24 to 48 registers of elements; 16 bytes of a column where they fit
+  return V * bytes == 16 ? (vpt >= 4 ? 1 : 4 / vpt) : (vpt >= 16 ? 1 : vpt == 8 ? 2 : vpt == 4 || bytes == 4 ? 4 : 8);
+}
+NormBwdShape norm_bwd_shape_of(const unipool_ctx* ctx, int T, int width, int v, bool aligned, int arrays) {
+  const int e = (int)ctx->elem_bytes, n = (width + v - 1) / v;
+  NormBwdShape s;
+  s.v = v;
+  s.vpt = n <= 512 ? 1 : n <= 1024 ? 2 : n <= 2048 ? 4 : n <= 4096 ? 8 : 32;
+  s.threads = ((n + s.vpt - 1) / s.vpt + 31) / 32 * 32;
+  s.rows = norm_bwd_rows(v, e, s.vpt);
+  const int64_t stage = (int64_t)s.rows * width * e * arrays;
+  int per_sm = s.threads <= 320 ? 640 / s.threads : 1;
+  per_sm = per_sm > 16 ? 16 : per_sm;
+  s.stages = 0;
+  if (aligned && (int64_t)s.rows * width * e % 16 == 0 && s.vpt <= 8) {
+    auto fit = [&](int blocks) { return (int)((220 * 1024 / blocks - 2304) / stage); };     // (2304: barriers, sums, the system's)
+    while (per_sm > 1 && fit(per_sm) < 2) --per_sm;
+    s.stages = fit(per_sm) > 4 ? 4 : fit(per_sm) < 2 ? 0 : fit(per_sm);
+  }
+  s.smem = s.stages > 0 ? (uint32_t)(s.stages * stage + 64) : 0;
+  const int all = (T + s.rows - 1) / s.rows, most = ctx->sm_count * per_sm;
+  s.blocks = all < most ? all : most;
+  return s;
+}
+NormBwdShape norm_bwd_shape(const unipool_ctx* ctx, int T, int width, bool aligned, int arrays) {
+  const int e = (int)ctx->elem_bytes;
+  if (aligned && width * e % 16 == 0) return norm_bwd_shape_of(ctx, T, width, 16 / e, true, arrays);
+  if (aligned && width % 2 == 0) {
+    const NormBwdShape s = norm_bwd_shape_of(ctx, T, width, 2, true, arrays);
+    if (s.stages > 0) return s;
+  }
+  return norm_bwd_shape_of(ctx, T, width, 1, aligned, arrays);
 }
 
 // Calls f(TPR, VPT) as compile-time numbers for rows of `n` vectors.
@@ -347,39 +482,55 @@ template <bool kNorm, typename E> int norm_as(unipool_ctx* ctx, const NormParams
   });
 }
 
-// Blocks of the backward kernel: up to two to an SM, each with a row for every warp.
-int norm_bwd_blocks(const unipool_ctx* ctx, int T, int rows) {
-  const int most = 2 * ctx->sm_count, all = (T + rows - 1) / rows;
-  return all < most ? all : most;
+template <typename E, int V, int VPT, bool kRing>
+int norm_bwd_run(const NormBwdShape& f, const NormBwdParams& p, cudaStream_t s) {
+  auto kern = rmsnorm_bwd_kernel<E, V, VPT, norm_bwd_rows(V, (int)sizeof(E), VPT), kRing>;
+  if (kRing) UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 223 * 1024));
+  UP_KERNEL(kern, f.blocks, f.threads, f.smem, s, p);
+  return UNIPOOL_OK;
 }
 
-template <typename E> int norm_bwd_as(unipool_ctx* ctx, NormBwdParams p, float* scratch, bool overwrite, cudaStream_t s) {
-  const uintptr_t rows = reinterpret_cast<uintptr_t>(p.dh) | reinterpret_cast<uintptr_t>(p.r) | reinterpret_cast<uintptr_t>(p.dr) |
-                         reinterpret_cast<uintptr_t>(p.dx) | reinterpret_cast<uintptr_t>(p.w);
-  const bool vec = (int64_t)p.width * sizeof(E) % 16 == 0 && rows % 16 == 0;
-  return by_row<E>(vec, p.width, [&](auto e, auto v, auto tpr, auto vpt) {
-    constexpr int kRows = kNormBwdThreads<tpr> / tpr;
-    const int blocks = norm_bwd_blocks(ctx, p.T, kRows);
-    float* dw = p.dw;
-    const bool split = dw != nullptr && blocks > 1;
-    NormBwdParams a = p;
-    a.add = !overwrite && !split;
-    if (split) a.dw = scratch;
-    PhaseTimer pt(ctx, UNIPOOL_PH_RMSNORM_BWD, split ? 2 : 1, s);
-    auto kern = rmsnorm_bwd_kernel<decltype(e), v, tpr, vpt>;
-    UP_KERNEL(kern, blocks, kNormBwdThreads<tpr>, tpr == 32 ? p.width * sizeof(float) : 0, s, a);
-    return split ? column_sum_launch(scratch, blocks, p.width, dw, !overwrite, s) : UNIPOOL_OK;
-  });
+template <typename E> int norm_bwd_as(unipool_ctx* ctx, NormBwdParams p, bool aligned, float* scratch, bool overwrite, cudaStream_t s) {
+  constexpr int V = 16 / (int)sizeof(E);
+  const NormBwdShape f = norm_bwd_shape(ctx, p.T, p.width, aligned, p.dr != nullptr ? 3 : 2);
+  float* dw = p.dw;
+  const bool split = dw != nullptr && f.blocks > 1;
+  p.add = !overwrite && !split;
+  p.stages = f.stages;
+  if (split) p.dw = scratch;
+  PhaseTimer pt(ctx, UNIPOOL_PH_RMSNORM_BWD, split ? 2 : 1, s);
+  auto by_vpt = [&](auto v, auto ring) {
+    constexpr int kV = decltype(v)::value;
+    constexpr bool kRing = decltype(ring)::value;
+    if (f.vpt == 1) return norm_bwd_run<E, kV, 1, kRing>(f, p, s);
+    if (f.vpt == 2) return norm_bwd_run<E, kV, 2, kRing>(f, p, s);
+    if (f.vpt == 4) return norm_bwd_run<E, kV, 4, kRing>(f, p, s);
+    if constexpr (kV <= 4) {                             // (no row has so many vectors of eight)
+      if (f.vpt == 8) return norm_bwd_run<E, kV, 8, kRing>(f, p, s);
+    }
+    if constexpr (kV == 1 && !kRing) return norm_bwd_run<E, 1, 32, false>(f, p, s);
+    return (int)UNIPOOL_ERR_UNSUPPORTED;
+  };
+  int rc;
+  if (f.stages > 0) rc = f.v == V ? by_vpt(Int<V>(), std::true_type()) : f.v == 1 ? by_vpt(Int<1>(), std::true_type()) : by_vpt(Int<2>(), std::true_type());
+  else if (f.v == 1) rc = by_vpt(Int<1>(), std::false_type());
+  else if constexpr (V == 4) rc = norm_bwd_run<E, 4, 8, false>(f, p, s);   // fp32 rows of 9472 and more: two do not fit
+  else rc = UNIPOOL_ERR_UNSUPPORTED;                     // (every bf16 row's do)
+  return rc == UNIPOOL_OK && split ? column_sum_launch(scratch, f.blocks, p.width, dw, !overwrite, s) : rc;
 }
 
 }  // namespace
 
 int norm_max_width() { return kNormMaxWidth; }
 
-// (The most blocks that any width and alignment takes.)
+// (The most that any alignment and number of arrays takes.)
 size_t rmsnorm_bwd_scratch(const unipool_ctx* ctx, int T, int width) {
-  const int most = 2 * ctx->sm_count;
-  return (size_t)(T < most ? T : most) * width * sizeof(float);
+  int most = 0;
+  for (int k = 0; k < 4; ++k) {
+    const int n = norm_bwd_shape(ctx, T, width, (k & 1) != 0, k < 2 ? 2 : 3).blocks;
+    most = n > most ? n : most;
+  }
+  return (size_t)most * width * sizeof(float);
 }
 
 int rmsnorm_launch(unipool_ctx* ctx, const void* x, const void* y, int T, int width, const float* w, float eps, void* r,
@@ -401,9 +552,11 @@ int rmsnorm_bwd_launch(unipool_ctx* ctx, const void* dh, const void* r, int T, i
     if (dw != nullptr && overwrite) UP_CUDA(cudaMemsetAsync(dw, 0, (size_t)width * sizeof(float), s));
     return UNIPOOL_OK;
   }
-  const NormBwdParams p{dh, r, dr, w, rstd, dx, dw, T, width, false};
-  return ctx->cfg.dtype == UNIPOOL_BF16 ? norm_bwd_as<__nv_bfloat16>(ctx, p, scratch, overwrite, s)
-                                        : norm_bwd_as<float>(ctx, p, scratch, overwrite, s);
+  const NormBwdParams p{dh, r, dr, w, rstd, dx, dw, T, width, 0, false, ctx->ws.status};
+  const uintptr_t all = reinterpret_cast<uintptr_t>(dh) | reinterpret_cast<uintptr_t>(r) | reinterpret_cast<uintptr_t>(dr) |
+                        reinterpret_cast<uintptr_t>(dx) | reinterpret_cast<uintptr_t>(w);
+  return ctx->cfg.dtype == UNIPOOL_BF16 ? norm_bwd_as<__nv_bfloat16>(ctx, p, all % 16 == 0, scratch, overwrite, s)
+                                        : norm_bwd_as<float>(ctx, p, all % 16 == 0, scratch, overwrite, s);
 }
 
 }  // namespace unipool
