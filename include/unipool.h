@@ -332,6 +332,14 @@ typedef struct {
   void *dYp, *dGU, *dx;                      /* dx [2,T,d]: dx[0] holds the upstream gradient on entry of     */
                                              /* backward, dx[n_layers % 2] the gradient of x[0] on return     */
   float *dgate, *dW_gu, *dW_down, *dW_r, *dsigma;
+  /* Pre-normalised blocks, x_{l+1} = x_l + MoE_l(norm(x_l)) with unipool_rmsnorm of every layer's own weight: W_n not   */
+  /* NULL.  Everything of the layer, the saved activations too, then works on h in the place of x.                       */
+  const float* W_n;                          /* [L,d]                                                        */
+  float* dW_n;                               /* [L,d] float +=                                               */
+  void *h, *dh;                              /* [L,T,d] (recompute: one slot, rebuilt in backward); [T,d]     */
+  float* rstd;                               /* [L,T]                                                        */
+  void* norm_scratch;                        /* unipool_rmsnorm_bwd_scratch(ctx, T, d) bytes                 */
+  float norm_eps;
 } unipool_stack;
 
 #define UNIPOOL_STACK_NO_AUX       4   /* unipool_stack_backward without the balance loss's gradient      */
@@ -390,7 +398,7 @@ int unipool_quantize_rows(unipool_ctx* ctx, const void* x, int32_t rows, int32_t
 
 /* Dense product with its epilogue, for the layers beside the experts (projections, dense FFN layers):
  *   p = x W^T + bias,  y = act(p) + residual,
- * accumulated in fp32, each output rounded once.  n_in and n_out are multiples of 64, independent of d_model and
+ * accumulated in fp32, each output rounded once.  n_in and n_out are multiples of 64 up to 2^21, independent of d_model and
  * d_ff.
  * in : x [T,n_in]; W [n_out,n_in] (ctx dtype); bias [n_out] float or NULL; act UNIPOOL_ACT_*; residual [T,n_out]
  *      (ctx dtype) or NULL.

@@ -56,9 +56,10 @@ class Stack(ctypes.Structure):
     """unipool_stack: the arrays of a whole residual stack."""
     POINTERS = ("W_gu", "W_down", "W_r", "sigma", "bias", "x", "idx", "gate", "counts", "score_sum", "znorm", "z",
                 "offsets", "rows", "row_of", "token_of", "tile_expert", "Xp", "GU", "A", "Yp", "loss", "coef", "fbar",
-                "dYp", "dGU", "dx", "dgate", "dW_gu", "dW_down", "dW_r", "dsigma")
+                "dYp", "dGU", "dx", "dgate", "dW_gu", "dW_down", "dW_r", "dsigma", "W_n", "dW_n", "h", "dh", "rstd",
+                "norm_scratch")
     _fields_ = ([(n, ctypes.c_int32) for n in ("n_layers", "layers_per_group", "n_experts", "recompute", "wgrad_layers")]
-                + [(n, ctypes.c_void_p) for n in POINTERS])
+                + [(n, ctypes.c_void_p) for n in POINTERS] + [("norm_eps", ctypes.c_float)])
 
 
 class UniPoolError(RuntimeError):
@@ -305,7 +306,7 @@ class Context:
     def rmsnorm_bwd(self, dh, r, T, width, w, rstd, dr, dx, dw, flags=0, scratch=None):
         """``scratch``: a device tensor of unipool_rmsnorm_bwd_scratch() bytes; allocated per call if None."""
         if scratch is None and dw is not None:
-            scratch = self._scratch(lib().unipool_rmsnorm_bwd_scratch(self.handle, T, width))
+            scratch = self._scratch(self.rmsnorm_bwd_scratch(T, width))
         _check(lib().unipool_rmsnorm_bwd(self.handle, _p(dh), _p(r), T, width, _p(w), _p(rstd), _p(dr), _p(dx), _p(dw),
                                          _p(scratch), flags, _stream()))
 
@@ -324,9 +325,17 @@ class Context:
     def linear_bwd(self, dy, T, n_out, pre, act, x, n_in, W, dp, dx_residual, dx, dW, dbias, flags=0, scratch=None):
         """``scratch``: a device tensor of unipool_linear_bwd_scratch() bytes; allocated per call if None."""
         if scratch is None and (dW is not None or dbias is not None):
-            scratch = self._scratch(lib().unipool_linear_bwd_scratch(self.handle, T, n_in, n_out))
+            scratch = self._scratch(self.linear_bwd_scratch(T, n_in, n_out))
         _check(lib().unipool_linear_bwd(self.handle, _p(dy), T, n_out, _p(pre), act, _p(x), n_in, _p(W), _p(dp),
                                         _p(dx_residual), _p(dx), _p(dW), _p(dbias), _p(scratch), flags, _stream()))
+
+    def rmsnorm_bwd_scratch(self, T, width):
+        """Bytes that rmsnorm_bwd needs beside its results."""
+        return lib().unipool_rmsnorm_bwd_scratch(self.handle, T, width)
+
+    def linear_bwd_scratch(self, T, n_in, n_out):
+        """Bytes that linear_bwd needs beside its results."""
+        return lib().unipool_linear_bwd_scratch(self.handle, T, n_in, n_out)
 
     def _scratch(self, nbytes):
         """Device memory for one call: the allocator hands it on to later work of the same stream only."""

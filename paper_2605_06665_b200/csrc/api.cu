@@ -409,8 +409,7 @@ int unipool_route_bwd(unipool_ctx* ctx, const void* x, int32_t T, const float* W
 }
 
 #define CHECK_WIDTH(n)                                                                           \
-  UP_REQUIRE((n) >= 1 && (n) <= norm_max_width(), UNIPOOL_ERR_UNSUPPORTED, "width = %d outside [1, %d]", (int)(n), \
-             norm_max_width())
+  UP_REQUIRE((n) >= 1 && (n) <= kNormMaxWidth, UNIPOOL_ERR_UNSUPPORTED, "width = %d outside [1, %d]", (int)(n), kNormMaxWidth)
 
 int unipool_rmsnorm(unipool_ctx* ctx, const void* x, const void* y, int32_t T, int32_t width, const float* w, float eps,
                     void* r, float* rstd, void* h, uint8_t* q, float* q_scale, unipool_stream stream) {
@@ -447,8 +446,8 @@ int unipool_quantize_rows(unipool_ctx* ctx, const void* x, int32_t rows, int32_t
 }
 
 #define CHECK_FEATURES(n)                                                                        \
-  UP_REQUIRE((n) >= 64 && (n) <= (1 << 24) && (n) % 64 == 0, UNIPOOL_ERR_UNSUPPORTED,            \
-             #n " = %d must be a multiple of 64 (2^24 at most)", (int)(n))
+  UP_REQUIRE((n) >= 64 && (n) <= (1 << 21) && (n) % 64 == 0, UNIPOOL_ERR_UNSUPPORTED,            \
+             #n " = %d must be a multiple of 64 (2^21 at most)", (int)(n))
 #define CHECK_ACT(a)                                                                             \
   UP_REQUIRE((a) >= UNIPOOL_ACT_NONE && (a) <= UNIPOOL_ACT_GELU, UNIPOOL_ERR_INVALID_ARG, "act = %d", (int)(a))
 // (the tensor-core path moves these by TMA)

@@ -232,7 +232,7 @@ int guard_check_launch(unipool_ctx*, cudaStream_t);
 int calibrate_launch(unipool_ctx*, int n_experts, int top_k, int n_samples, uint64_t seed,
                      float* c_out, cudaStream_t);
 
-int norm_max_width();
+constexpr int kNormMaxWidth = 16384;          // columns of a row of the RMS norm: what 512 threads hold in registers
 int rmsnorm_launch(unipool_ctx*, const void* x, const void* y, int T, int width, const float* w, float eps, void* r,
                    float* rstd, void* h, uint8_t* q, float* q_scale, cudaStream_t);
 size_t rmsnorm_bwd_scratch(const unipool_ctx*, int T, int width);

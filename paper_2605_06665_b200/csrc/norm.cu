@@ -21,7 +21,6 @@ namespace unipool {
 
 namespace {
 
-constexpr int kNormMaxWidth = 16384;
 constexpr float kE4m3Max = 448.f;
 constexpr float kSmallestScale = 1.17549435e-38f;        // 2^-126: its reciprocal is finite, a row of zeros keeps zeros
 
@@ -520,8 +519,6 @@ template <typename E> int norm_bwd_as(unipool_ctx* ctx, NormBwdParams p, bool al
 }
 
 }  // namespace
-
-int norm_max_width() { return kNormMaxWidth; }
 
 // (The most that any alignment and number of arrays takes.)
 size_t rmsnorm_bwd_scratch(const unipool_ctx* ctx, int T, int width) {

@@ -40,6 +40,11 @@ struct Layer {
   int32_t* tile_expert() const { return at(s->tile_expert, l, cap / UNIPOOL_ROW_ALIGN); }
   float* znorm() const { return at(s->znorm, l, T); }
   float* z() const { return at(s->z, l, T * m); }
+  bool norm() const { return s->W_n != nullptr; }
+  const float* W_n() const { return at(s->W_n, l, d); }
+  float* dW_n() const { return at(s->dW_n, l, d); }
+  float* rstd() const { return at(s->rstd, l, T); }
+  void* h() const { return norm() ? at_bytes(s->h, slot(), T * d * eb) : x(l); }     // what the layer works on
   void* per_row(void* p, int sl, int64_t width) const { return at_bytes(p, sl, cap * width * eb); }
 };
 
@@ -54,14 +59,22 @@ int check_stack(const unipool_ctx* ctx, const unipool_stack* s) {
   UP_REQUIRE(s->n_layers >= 1 && s->n_layers <= ctx->cfg.n_layers && s->layers_per_group >= 1 &&
                  s->n_layers % s->layers_per_group == 0,
              UNIPOOL_ERR_INVALID_ARG, "stack of %d layers in groups of %d", s->n_layers, s->layers_per_group);
+  UP_REQUIRE(s->W_n == nullptr || (s->h != nullptr && s->rstd != nullptr), UNIPOOL_ERR_INVALID_ARG, "W_n without h or rstd");
   UP_REQUIRE(s->sigma != nullptr && s->x != nullptr, UNIPOOL_ERR_INVALID_ARG, "sigma or x is NULL");
   return UNIPOOL_OK;
+}
+
+// norm of a layer's input, if the stack has them
+int norm_layer(unipool_ctx* ctx, const Layer& a, int32_t T, unipool_stream stream) {
+  if (!a.norm()) return UNIPOOL_OK;
+  return unipool_rmsnorm(ctx, a.x(a.l), nullptr, T, ctx->cfg.d_model, a.W_n(), a.s->norm_eps, nullptr, a.rstd(), a.h(), nullptr,
+                         nullptr, stream);
 }
 
 // dispatch + expert forward of a layer; w: slot of Xp and A
 int permute_and_experts(unipool_ctx* ctx, const Layer& a, int32_t T, int w, unipool_stream stream) {
   const unipool_stack* s = a.s;
-  UP_TRY(unipool_dispatch_rows(ctx, a.x(a.l), T, a.idx(), s->n_experts, a.offsets(), a.row_of(), a.token_of(),
+  UP_TRY(unipool_dispatch_rows(ctx, a.h(), T, a.idx(), s->n_experts, a.offsets(), a.row_of(), a.token_of(),
                                a.tile_expert(), a.rows(), a.per_row(s->Xp, w, a.d), stream));
   return unipool_expert_fwd_rows(ctx, a.per_row(s->Xp, w, a.d), a.offsets(), a.rows(), a.tile_expert(), s->W_gu,
                                  s->W_down, a.base(), s->n_experts, a.per_row(s->GU, a.slot(), 2 * a.f),
@@ -84,7 +97,8 @@ int unipool_stack_forward(unipool_ctx* ctx, const unipool_stack* s, int32_t T, u
   UP_TRY(unipool_router_prepare(ctx, s->W_r, s->n_layers, s->n_experts, stream));
   for (int l = 0; l < s->n_layers; ++l) {
     const Layer a(ctx, s, l);
-    UP_TRY(unipool_route(ctx, a.x(l), T, a.W_r(), s->sigma[l], a.bias(), s->n_experts, a.idx(), a.gate(),
+    UP_TRY(norm_layer(ctx, a, T, stream));
+    UP_TRY(unipool_route(ctx, a.h(), T, a.W_r(), s->sigma[l], a.bias(), s->n_experts, a.idx(), a.gate(),
                          at(s->counts, l, a.m), at(s->score_sum, l, a.m), a.znorm(), a.z(), stream));
     UP_TRY(permute_and_experts(ctx, a, T, a.slot(), stream));
     UP_TRY(unipool_combine(ctx, a.per_row(s->Yp, a.slot(), a.d), a.row_of(), a.gate(), T, a.x(l), a.x(l + 1), stream));
@@ -108,6 +122,7 @@ int unipool_stack_backward(unipool_ctx* ctx, const unipool_stack* s, int32_t T, 
              UNIPOOL_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
   UP_REQUIRE(s->wgrad_layers >= 1 && s->dx != nullptr, UNIPOOL_ERR_INVALID_ARG, "wgrad_layers = %d, or dx is NULL",
              s->wgrad_layers);
+  UP_REQUIRE(s->W_n == nullptr || (s->dh != nullptr && s->dW_n != nullptr), UNIPOOL_ERR_INVALID_ARG, "W_n without dh or dW_n");
   const int lg = s->layers_per_group, overwrite = flags & UNIPOOL_WGRAD_OVERWRITE;
   const int run = s->wgrad_layers < lg ? s->wgrad_layers : lg;            // layers contracted together
   // operands of the layer's weight gradient: stacked over all layers, or slots of one run
@@ -120,16 +135,24 @@ int unipool_stack_backward(unipool_ctx* ctx, const unipool_stack* s, int32_t T, 
     const int b = stacked ? l : hold;                                     // dYp, dGU
     // the first contribution to a group's experts: its top layer, or the run that layer belongs to
     const int over = overwrite && i >= (lg - 1) / run * run ? UNIPOOL_WGRAD_OVERWRITE : 0;
-    if (s->recompute) UP_TRY(permute_and_experts(ctx, a, T, w, stream));
+    if (s->recompute) {
+      UP_TRY(norm_layer(ctx, a, T, stream));
+      UP_TRY(permute_and_experts(ctx, a, T, w, stream));
+    }
     void *dx_next = at_bytes(s->dx, cur, a.T * a.d * a.eb), *dx_out = at_bytes(s->dx, cur ^ 1, a.T * a.d * a.eb);
+    void* dh = a.norm() ? s->dh : dx_out;                                 // gradient of what the layer works on
     UP_TRY(unipool_expert_bwd_rows(ctx, dx_next, T, a.row_of(), a.gate(), a.token_of(), a.offsets(), a.rows(),
                                    a.tile_expert(), a.per_row(s->Xp, w, a.d), a.per_row(s->GU, a.slot(), 2 * a.f),
                                    a.per_row(s->A, w, a.f), a.per_row(s->Yp, a.slot(), a.d), s->W_gu, s->W_down, a.base(),
-                                   s->n_experts, dx_next, a.per_row(s->dYp, b, a.d), a.per_row(s->dGU, b, 2 * a.f), dx_out,
+                                   s->n_experts, a.norm() ? nullptr : dx_next, a.per_row(s->dYp, b, a.d),
+                                   a.per_row(s->dGU, b, 2 * a.f), dh,
                                    s->dgate, s->dW_gu, s->dW_down, run > 1 ? UNIPOOL_BWD_SKIP_WGRAD : over, stream));
-    UP_TRY(unipool_route_bwd(ctx, a.x(l), T, a.W_r(), s->sigma[l], s->n_experts, a.znorm(), a.z(), a.idx(), s->dgate,
-                             (flags & UNIPOOL_STACK_NO_AUX) ? nullptr : at(s->coef, l / lg, a.m), dx_out, a.dW_r(),
+    UP_TRY(unipool_route_bwd(ctx, a.h(), T, a.W_r(), s->sigma[l], s->n_experts, a.znorm(), a.z(), a.idx(), s->dgate,
+                             (flags & UNIPOOL_STACK_NO_AUX) ? nullptr : at(s->coef, l / lg, a.m), dh, a.dW_r(),
                              at(s->dsigma, l, 1), stream));
+    if (a.norm())
+      UP_TRY(unipool_rmsnorm_bwd(ctx, dh, a.x(l), T, ctx->cfg.d_model, a.W_n(), a.rstd(), dx_next, dx_out, a.dW_n(),
+                                 s->norm_scratch, 0, stream));
     if (run > 1 && !stacked && hold == 0)                                 // the lowest layer of a run
       UP_TRY(unipool_pool_wgrad_rows(ctx, run < lg - i ? run : lg - i, a.cap, a.offsets(), a.rows(), s->Xp, s->A, s->dYp,
                                      s->dGU, a.base(), s->n_experts, s->dW_gu, s->dW_down, over, stream));

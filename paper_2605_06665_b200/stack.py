@@ -20,6 +20,11 @@ the private layout).  In the private layout the
 balance loss is the per-layer loss of Eq. 3 summed over layers.  ``router="softmax"``
 replaces the NormRouter of Eq. 7 by the conventional softmax router of the paper's
 baselines (Sec. 5.1) in every layer.
+
+``norm=True`` makes the blocks pre-normalised as in the paper's backbone (App. B, App. D):
+x_{l+1} = x_l + MoE_l(norm(x_l)) with a root-mean-square norm of every layer's own weight ``W_n[l]``
+(ones at the start); router, permute and experts then read ``h[l]`` = norm(x_l), and backward adds the norms'
+weight gradients into ``dW_n`` beside the routers'.
 """
 from __future__ import annotations
 
@@ -34,7 +39,7 @@ from . import binding as B
 class UniPoolStack:
     def __init__(self, L, d, f, M, k, T, dtype="bf16", private=0, c=1.0, eps=1e-6, alpha=1e-2,
                  device="cuda", deferred_wgrad=False, recompute=False, groups=None, router="norm",
-                 wgrad_layers=None):
+                 wgrad_layers=None, norm=False, norm_eps=1e-6):
         self.L, self.d, self.f, self.M, self.k, self.T = L, d, f, M, k, T
         if groups is None:
             groups = L if private else 1
@@ -95,6 +100,13 @@ class UniPoolStack:
         self.Yp = e(ns, cap, d)
         self.dx = e(2, T, d)                               # ping-pong dx_{l+1} -> dx_l
         self.dgate = e(T, k, dtype=f32)
+        # norms in front of the layers (h and rstd are kept for backward; recompute rebuilds h in one slot)
+        self.norm, self.norm_eps = norm, norm_eps
+        self.W_n = torch.ones(L, d, dtype=f32, device=dev) if norm else None
+        self.dW_n = torch.zeros(L, d, dtype=f32, device=dev) if norm else None
+        self.h, self.dh = (e(ns, T, d), e(T, d)) if norm else (None, None)
+        self.rstd = e(L, T, dtype=f32) if norm else None
+        self.norm_scratch = e(self.ctx.rmsnorm_bwd_scratch(T, d), dtype=torch.uint8) if norm else None
         # balance loss
         n_aux = groups                                     # one balance loss per sharing group
         self.loss = torch.zeros(n_aux, dtype=f32, device=dev)
@@ -111,7 +123,8 @@ class UniPoolStack:
                 raise
             self.nw = 1
             self._make_operands(e)
-        self._stacked = [(n, getattr(self, n).numel()) for n in B.Stack.POINTERS if n not in ("sigma", "bias")]
+        self._stacked = [(n, getattr(self, n).numel()) for n in B.Stack.POINTERS
+                         if n not in ("sigma", "bias") and getattr(self, n) is not None]
 
     def _make_operands(self, e):
         self.Xp = self.A = self.dYp = self.dGU = None
@@ -158,17 +171,23 @@ class UniPoolStack:
         return 0 if self.recompute else l
 
     def zero_grad(self):
-        self.dW_gu.zero_(); self.dW_down.zero_(); self.dW_r.zero_(); self.dsigma.zero_()
+        self.dW_gu.zero_(); self.dW_down.zero_()
+        self.zero_router_grad()
 
     def zero_router_grad(self):
+        """The gradients that every pass adds into: the routers' and the norms'."""
         self.dW_r.zero_(); self.dsigma.zero_()
+        if self.norm:
+            self.dW_n.zero_()
 
     def _arrays(self):
         """This stack's arrays as they are now, for the calls that run all layers; None if one of them is not
         a dense array over the layers.  (Arrays that were given up, as an evaluation may those of backward, are NULL:
         a call that needs them refuses them.)"""
+        if self.norm and self.W_n is None:
+            raise ValueError("a stack with norms needs W_n")
         wgrad = self.Lg if self.deferred_wgrad else self.nw
-        s = B.Stack(self.L, self.Lg, self.m, int(self.recompute), wgrad)
+        s = B.Stack(self.L, self.Lg, self.m, int(self.recompute), wgrad, norm_eps=self.norm_eps)
         try:
             for n, numel in self._stacked:
                 t = getattr(self, n)
@@ -206,16 +225,26 @@ class UniPoolStack:
     def forward_layer(self, l, T=None):
         T = self.T if T is None else T
         c = self.ctx
-        c.route(self.x[l], T, self.W_r[l], self.sigma[l], self._bias(l), self.m, self.idx[l], self.gate[l],
+        self.norm_layer(l, T)
+        c.route(self._input(l), T, self.W_r[l], self.sigma[l], self._bias(l), self.m, self.idx[l], self.gate[l],
                 self.counts[l], self.score_sum[l], self.znorm[l], self.z[l])
         self.permute_and_experts(l, T)
         c.combine(self.Yp[self.slot(l)], self.row_of[l], self.gate[l], T, self.x[l], self.x[l + 1])
 
+    def norm_layer(self, l, T):
+        """h and rstd of layer l from x_l (nothing in a stack without norms)."""
+        if self.norm:
+            self.ctx.rmsnorm(self.x[l], None, T, self.d, self.W_n[l], self.norm_eps, None, self.rstd[l], self._input(l))
+
+    def _input(self, l):
+        """What layer l works on."""
+        return self.h[self.slot(l)] if self.norm else self.x[l]
+
     def permute_and_experts(self, l, T):
-        """dispatch + expert forward of layer l from x_l and its routing decision (also the
+        """dispatch + expert forward of layer l from its input and its routing decision (also the
         recompute step of backward)."""
         c, s = self.ctx, self.slot(l)
-        c.dispatch(self.x[l], T, self.idx[l], self.m, self.offsets[l], self.row_of[l], self.token_of[l],
+        c.dispatch(self._input(l), T, self.idx[l], self.m, self.offsets[l], self.row_of[l], self.token_of[l],
                    self.tile_expert[l], self.Xp[s], self.rows[l])
         c.expert_fwd(self.Xp[s], self.offsets[l], self.tile_expert[l], self.W_gu, self.W_down,
                      self.base(l), self.m, self.GU[s], self.A[s], self.Yp[s], self.rows[l])
@@ -266,17 +295,22 @@ class UniPoolStack:
         s = l if self.deferred_wgrad else 0
         a = self.slot(l)
         if self.recompute:
+            self.norm_layer(l, T)
             self.permute_and_experts(l, T)
+        dh = self.dh if self.norm else dx_out              # gradient of what the layer works on
         flags = B.BWD_SKIP_WGRAD if self.deferred_wgrad else (B.WGRAD_OVERWRITE if overwrite else 0)
         c.expert_bwd(dx_next, T, self.row_of[l], self.gate[l], self.token_of[l], self.offsets[l],
                      self.tile_expert[l], self.Xp[a], self.GU[a], self.A[a], self.Yp[a], self.W_gu,
-                     self.W_down, self.base(l), self.m, dx_next, self.dYp[s], self.dGU[s], dx_out,
+                     self.W_down, self.base(l), self.m, None if self.norm else dx_next, self.dYp[s], self.dGU[s], dh,
                      self.dgate, self.dW_gu, self.dW_down, flags)
         coef = None
         if with_aux:
             coef = self.coef[l // self.Lg]
-        c.route_bwd(self.x[l], T, self.W_r[l], self.sigma[l], self.m, self.znorm[l], self.z[l],
-                    self.idx[l], self.dgate, coef, dx_out, self.dW_r[l], self.dsigma[l:l + 1])
+        c.route_bwd(self._input(l), T, self.W_r[l], self.sigma[l], self.m, self.znorm[l], self.z[l],
+                    self.idx[l], self.dgate, coef, dh, self.dW_r[l], self.dsigma[l:l + 1])
+        if self.norm:
+            c.rmsnorm_bwd(dh, self.x[l], T, self.d, self.W_n[l], self.rstd[l], dx_next, dx_out, self.dW_n[l],
+                          scratch=self.norm_scratch)
 
     def backward(self, upstream=None, T=None, with_aux=True, accumulate=True, exchange=None):
         """``accumulate=False``: the pool gradient of this pass replaces the buffers' contents
@@ -316,7 +350,7 @@ class UniPoolStack:
         if exchange is not None:
             if not self.deferred_wgrad:
                 exchange.launch([self.dW_down, self.dW_gu])
-            exchange.launch([self.dW_r, self.dsigma])
+            exchange.launch([self.dW_r, self.dsigma] + ([self.dW_n] if self.norm else []))
             exchange.finish()
         return self.dx[self.L % 2]
 

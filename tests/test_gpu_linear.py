@@ -431,3 +431,33 @@ def test_dense_block_in_eight_bits():
     assert (out.double() - full).norm() <= 4 * 2.0 ** -4 / 3 ** 0.5 * path.norm() + half_step(m.dt) * 2 * full.norm()
     c.check_status()
     c.close()
+
+
+def test_more_than_32_bits_of_elements():
+    """17000 tokens of 131072 features: the last ones lie 2.2e9 elements behind the first, in the result, the residual and dp."""
+    from paper_2605_06665_b200 import binding as B
+    T, n_in, n_out, dt = 17_000, 64, 131_072, torch.bfloat16
+    ctx = B.Context(B.make_config(64, 64, 1, 1, 1, T, B.BF16, 1e-6, 1.0))
+    x, W, bias = normal((T, n_in), dt, 70), normal((n_out, n_in), dt, 71, 0.1), normal((n_out,), torch.float32, 72)
+    rows = [0, 255, 16383, 16384, 16385, T - 1]
+    y = torch.zeros(T, n_out, dtype=dt, device="cuda")
+    y[rows] = normal((len(rows), n_out), dt, 73)
+    res = y[rows].double()
+    ctx.linear(x, T, n_in, W, n_out, bias, 0, y, None, y)
+    want = x[rows].double() @ W.double().T + bias.double() + res
+    terms = x[rows].double().abs() @ W.double().abs().T + bias.double().abs() + res.abs()
+    assert ((y[rows].double() - want).abs() <= half_step(dt) * 1.001 * want.abs() + 2.0 ** -24 * 48 * terms).all()
+    dx, dW = torch.empty_like(x), torch.empty(n_out, n_in, device="cuda")
+    keep = torch.zeros(T, dtype=torch.bool, device="cuda")
+    keep[rows] = True
+    y[~keep] = 0
+    db = torch.empty(n_out, device="cuda")
+    ctx.linear_bwd(y, T, n_out, None, 0, x, n_in, W, None, None, dx, dW, db, B.WGRAD_OVERWRITE)
+    g = y[rows].double()
+    want, terms = g @ W.double(), g.abs() @ W.double().abs()
+    assert ((dx[rows].double() - want).abs() <= half_step(dt) * 1.001 * want.abs() + 2.0 ** -24 * 2 * (n_out / 16 + 16) * terms).all()
+    want, terms = g.T @ x[rows].double(), g.abs().T @ x[rows].double().abs()
+    assert ((dW.double() - want).abs() <= 2.0 ** -24 * 500 * terms).all()
+    assert ((db.double() - g.sum(0)).abs() <= 64 * 2.0 ** -24 * g.abs().sum(0)).all()
+    ctx.check_status()
+    ctx.close()

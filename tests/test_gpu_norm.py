@@ -289,3 +289,24 @@ def test_captured_and_on_another_stream(mode):
             assert torch.equal(out[0], want[0]) and torch.equal(out[1], want[1])
             out[0].zero_(), out[1].zero_()
         torch.cuda.synchronize()
+
+
+def test_more_than_32_bits_of_elements():
+    """135000 rows of 16384: the last rows lie 2.2e9 elements behind the first."""
+    from paper_2605_06665_b200 import binding as B
+    T, width, dt = 135_000, 16384, torch.bfloat16
+    ctx = B.Context(B.make_config(64, 64, 1, 1, 1, T, B.BF16, EPS, 1.0))
+    x, w = torch.zeros(T, width, dtype=dt, device="cuda"), 1 + normal((width,), torch.float32, 40, 0.2)
+    rows = [0, 1, 131071, 131072, 131073, T - 2, T - 1]
+    x[rows] = normal((len(rows), width), dt, 41)
+    h, rstd = torch.empty_like(x), torch.empty(T, device="cuda")
+    ctx.rmsnorm(x, None, T, width, w, EPS, None, rstd, h)
+    rr, rs, hh = reference(x[rows], None, w, EPS)
+    assert ((h[rows].double() - hh).abs() <= (half_step(dt) + FP32) * hh.abs()).all()
+    dw, dw1, dx1 = torch.empty(width, device="cuda"), torch.empty(width, device="cuda"), torch.empty(len(rows), width, dtype=dt, device="cuda")
+    ctx.rmsnorm_bwd(x, x, T, width, w, rstd, None, h, dw, B.WGRAD_OVERWRITE)
+    ctx.rmsnorm_bwd(x[rows], x[rows], len(rows), width, w, rstd[rows], None, dx1, dw1, B.WGRAD_OVERWRITE)
+    assert torch.equal(h[rows], dx1)
+    assert ((dw - dw1).abs() <= 16 * 2.0 ** -24 * (x[rows].double() ** 2 * rs[:, None]).sum(0)).all()     # seven terms, in another order
+    ctx.check_status()
+    ctx.close()
