@@ -340,7 +340,7 @@ class Context:
     def _scratch(self, nbytes):
         """Device memory for one call: the allocator hands it on to later work of the same stream only."""
         import torch
-        return torch.empty(max(nbytes, 16), dtype=torch.uint8, device=self.device)
+        return torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
 
     def unique_experts(self, idx, expert_base, L, T, unique, total):
         _check(lib().unipool_unique_experts(self.handle, _p(idx), _p(expert_base), L, T, _p(unique), _p(total),

@@ -432,7 +432,7 @@ int unipool_rmsnorm_bwd(unipool_ctx* ctx, const void* dh, const void* r, int32_t
   CHECK_CTX(ctx); CHECK_T(ctx, T); CHECK_WIDTH(width);
   CHECK_PTR(dh); CHECK_PTR(r); CHECK_PTR(w); CHECK_PTR(rstd); CHECK_PTR(dx);
   UP_REQUIRE((flags & ~UNIPOOL_WGRAD_OVERWRITE) == 0, UNIPOOL_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
-  if (dw != nullptr && T > 0) CHECK_SCRATCH(scratch);
+  if (dw != nullptr && T > 0 && rmsnorm_bwd_scratch(ctx, T, width) > 0) CHECK_SCRATCH(scratch);
   return rmsnorm_bwd_launch(ctx, dh, r, T, width, w, rstd, dr, dx, dw, static_cast<float*>(scratch),
                             (flags & UNIPOOL_WGRAD_OVERWRITE) != 0, static_cast<cudaStream_t>(stream));
 }
@@ -494,7 +494,7 @@ int unipool_linear_bwd(unipool_ctx* ctx, const void* dy, int32_t T, int32_t n_ou
   UP_REQUIRE((flags & ~UNIPOOL_WGRAD_OVERWRITE) == 0, UNIPOOL_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
   if (dx != nullptr) CHECK_PTR(W);
   if (dW != nullptr) CHECK_PTR(x);
-  if ((dW != nullptr || dbias != nullptr) && T > 0) CHECK_SCRATCH(scratch);
+  if ((dW != nullptr || dbias != nullptr) && T > 0 && linear_bwd_scratch(ctx, T, n_in, n_out) > 0) CHECK_SCRATCH(scratch);
   CHECK_ALIGNED(ctx, dy); CHECK_ALIGNED(ctx, pre); CHECK_ALIGNED(ctx, dp); CHECK_ALIGNED(ctx, x); CHECK_ALIGNED(ctx, W);
   CHECK_ALIGNED(ctx, dx_residual); CHECK_ALIGNED(ctx, dx); CHECK_ALIGNED(ctx, dW);
   LinearBwdArgs a{dy, pre, x, W, T, n_in, n_out, act, dp, dx_residual, dx, dW, dbias, static_cast<float*>(scratch),

@@ -2,6 +2,8 @@
 // kernels beside both paths.
 //   forward   p = x W^T + bias,  y = act(p) + residual
 //   backward  dp = dy act'(p),  dx = dp W (+ dx_residual),  dW (+)= dp^T x,  dbias (+)= sum_t dp
+#include <cooperative_groups.h>
+
 #include <type_traits>
 
 #include "common.cuh"
@@ -79,9 +81,11 @@ __global__ void __launch_bounds__(256) linear_dp_kernel(DpParams a) {
 
 // Rows of each of n row blocks: whole steps of the loop.
 int dp_rows(int T, int n) { return ((T + n - 1) / n + kDpRows * kDpAhead - 1) / (kDpRows * kDpAhead) * (kDpRows * kDpAhead); }
-// Row blocks of the kernel: so many that four blocks lie on an SM, of 32 rows at least.
+// Row blocks of the kernel: so many that four blocks lie on an SM, of 32 rows at least; few rows on one, which leaves nothing to
+// add up behind it.
 int dp_row_blocks(const unipool_ctx* ctx, int T, int N, int cols_per_block) {
   const int across = (N + cols_per_block - 1) / cols_per_block;
+  if (T <= 3 * kDpRows * kDpAhead) return 1;
   int n = 4 * ctx->sm_count / across;
   if (n > (T + 31) / 32) n = (T + 31) / 32;
   if (n < 1) n = 1;
@@ -89,43 +93,49 @@ int dp_row_blocks(const unipool_ctx* ctx, int T, int N, int cols_per_block) {
 }
 
 // ---------------------------------------------------------------- sums of parts, in their order
-// out (+)= sum over the parts.  Few parts of many columns (a weight gradient's): a thread sums four columns, 16 bytes at a time.
-__global__ void __launch_bounds__(256) part_sum_kernel(const float* parts, int n_parts, int64_t width, float* out, bool add) {
-  grid_wait(parts);
-  const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
-  if (c >= width) return;
-  float4 v = __ldg(reinterpret_cast<const float4*>(parts + c));
+// out [width] (+)= the sum over n parts [n, width].
+struct PartSum { const float* parts; int n; int64_t width; float* out; bool add; };
+
+// Blocks [0, wide_blocks): few parts of many columns (a weight gradient's), four columns to a thread, 16 bytes at a time.  The others:
+// many parts of few columns, eight columns, a sector, to a block, whose 32 groups of eight threads take every 32nd part.
+__global__ void __launch_bounds__(256) part_sum_kernel(PartSum wide, int wide_blocks, PartSum tall) {
+  grid_wait(wide.parts, tall.parts);
+  if ((int)blockIdx.x < wide_blocks) {
+    const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
+    if (c >= wide.width) return;
+    float4 v = __ldg(reinterpret_cast<const float4*>(wide.parts + c));
 #pragma unroll 4
-  for (int i = 1; i < n_parts; ++i) {
-    const float4 o = __ldg(reinterpret_cast<const float4*>(parts + i * width + c));
-    v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+    for (int i = 1; i < wide.n; ++i) {
+      const float4 o = __ldg(reinterpret_cast<const float4*>(wide.parts + i * wide.width + c));
+      v.x += o.x; v.y += o.y; v.z += o.z; v.w += o.w;
+    }
+    float* out = &wide.out[c];
+    if (wide.add) v = make_float4(v.x + out[0], v.y + out[1], v.z + out[2], v.w + out[3]);
+    st4(out, v, (reinterpret_cast<uintptr_t>(out) & 15) == 0);
+    return;
   }
-  if (add) {
-    out[c] += v.x; out[c + 1] += v.y; out[c + 2] += v.z; out[c + 3] += v.w;
-  } else {
-    out[c] = v.x; out[c + 1] = v.y; out[c + 2] = v.z; out[c + 3] = v.w;
-  }
-}
-// Many parts of few columns: eight columns, a sector, to a block, whose 32 groups of eight threads take every 32nd part.
-__global__ void __launch_bounds__(256) column_sum_kernel(const float* parts, int n_parts, int64_t width, float* out, bool add) {
-  grid_wait(parts);
   __shared__ float s[8][8];
   const int lane = threadIdx.x % 32, g = threadIdx.x / 8;
-  const int64_t c = (int64_t)blockIdx.x * 8 + threadIdx.x % 8;
+  const int64_t c = (int64_t)(blockIdx.x - wide_blocks) * 8 + threadIdx.x % 8;
   float v = 0.f;
-  if (c < width) {
+  if (c < tall.width) {
 #pragma unroll 8
-    for (int i = g; i < n_parts; i += 32) v += __ldg(parts + i * width + c);
+    for (int i = g; i < tall.n; i += 32) v += __ldg(tall.parts + i * tall.width + c);
   }
   v += __shfl_xor_sync(0xffffffffu, v, 8);
   v += __shfl_xor_sync(0xffffffffu, v, 16);
   if (lane < 8) s[threadIdx.x / 32][lane] = v;
   __syncthreads();
-  if (threadIdx.x >= 8 || c >= width) return;
+  if (threadIdx.x >= 8 || c >= tall.width) return;
   v = s[0][lane];
 #pragma unroll
   for (int i = 1; i < 8; ++i) v += s[i][lane];
-  out[c] = add ? out[c] + v : v;
+  tall.out[c] = tall.add ? tall.out[c] + v : v;
+}
+int part_sum(const PartSum& wide, const PartSum& tall, cudaStream_t s) {       // (one of n = 0: none)
+  const int a = wide.n > 0 ? (int)((wide.width / 4 + 255) / 256) : 0, b = tall.n > 0 ? (int)((tall.width + 7) / 8) : 0;
+  if (a + b > 0) UP_KERNEL(part_sum_kernel, a + b, 256, 0, s, wide, a, tall);
+  return UNIPOOL_OK;
 }
 
 // ---------------------------------------------------------------- fp32 products on CUDA cores
@@ -138,21 +148,25 @@ struct SimtLinear {
   bool vec_a, vec_b, vec_c, add;                         // 16-byte aligned operands; vec_c: everything of the epilogue
 };
 
-// C = act(A B + bias) + residual; B along K (forward) or across it (dx).
-template <typename Tile, Major BM>
-__global__ void __launch_bounds__(Tile::kThreads, Tile::kBlocks) linear_rows_kernel(SimtLinear p) {
+// C = act(A B + bias) + residual; B along K (forward) or across it (dx).  S blocks of a cluster share a tile by taking runs of its
+// contraction and add up through each other's shared memory, in the order of their ranks (few tiles of a long contraction leave
+// most SMs idle otherwise: 16 tokens 2048 -> 1728 35 us with one block to a tile, XX with eight).
+template <typename Tile, Major BM, int S>
+__global__ void __cluster_dims__(1, 1, S) __launch_bounds__(Tile::kThreads, Tile::kBlocks) linear_rows_kernel(SimtLinear p) {
   grid_wait(p.A, p.B, p.bias, p.residual);
   extern __shared__ float4 smem_raw[];
   typename Tile::Smem& sm = *reinterpret_cast<typename Tile::Smem*>(smem_raw);
   const int m0 = blockIdx.x * Tile::kRows, n0 = blockIdx.y * kSimtN;
+  const int all = p.K / kSimtKC, c0 = all * (int)blockIdx.z / S, c1 = all * ((int)blockIdx.z + 1) / S;
   Tile t;
   t.template run<kAlongK, BM>(
-      sm, p.K / kSimtKC, p.vec_a, p.vec_b, p.A, [](int) {},
-      [&](int c, int i, int k) { return m0 + i < p.M ? p.A + (int64_t)(m0 + i) * p.K + c * kSimtKC + k : nullptr; },
+      sm, c1 - c0, p.vec_a, p.vec_b, p.A, [](int) {},
+      [&](int c, int i, int k) { return m0 + i < p.M ? p.A + (int64_t)(m0 + i) * p.K + (c0 + c) * kSimtKC + k : nullptr; },
       [&](int c, int i, int k) {
-        return BM == kAlongK ? p.B + (int64_t)(n0 + i) * p.K + c * kSimtKC + k : p.B + (int64_t)(c * kSimtKC + k) * p.N + n0 + i;
+        const int kk = (c0 + c) * kSimtKC + k;
+        return BM == kAlongK ? p.B + (int64_t)(n0 + i) * p.K + kk : p.B + (int64_t)kk * p.N + n0 + i;
       });
-  t.each4(sm, [&](int i, int j, float4 v) {
+  auto put = [&](int i, int j, float4 v) {
     if (m0 + i >= p.M) return;
     const int n = n0 + j;
     const int64_t at = (int64_t)(m0 + i) * p.N + n;
@@ -170,7 +184,29 @@ __global__ void __launch_bounds__(Tile::kThreads, Tile::kBlocks) linear_rows_ker
       v = make_float4(v.x + b.x, v.y + b.y, v.z + b.z, v.w + b.w);
     }
     st4(p.C + at, v, p.vec_c);
-  });
+  };
+  if constexpr (S == 1) {
+    t.each4(sm, put);
+  } else {
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    float* mine = sm.w[0].sums;
+    t.each4(sm, [&](int i, int j, float4 v) { *reinterpret_cast<float4*>(&mine[i * kSimtLd + j]) = v; });
+    cluster.sync();
+    constexpr int kQuads = Tile::kRows * kSimtN / 4;
+    for (int q = kQuads / S * (int)blockIdx.z + threadIdx.x; q < kQuads / S * ((int)blockIdx.z + 1); q += Tile::kThreads) {
+      const int i = q / (kSimtN / 4), j = q % (kSimtN / 4) * 4;
+      float4 part[S];
+#pragma unroll
+      for (int o = 0; o < S; ++o) part[o] = *reinterpret_cast<const float4*>(&cluster.map_shared_rank(mine, o)[i * kSimtLd + j]);
+#pragma unroll
+      for (int o = 1; o < S; ++o) {
+        part[0].x += part[o].x; part[0].y += part[o].y; part[0].z += part[o].z; part[0].w += part[o].w;
+      }
+      put(i, j, part[0]);
+    }
+    cluster.sync();                                      // no block leaves while another reads its sums
+  }
 }
 
 // C [M, N] (+)= sum over the tokens of a part of A[t, m] B[t, n]; part z of C behind the one before it.
@@ -199,19 +235,28 @@ __global__ void __launch_bounds__(LinearDwTile::kThreads, LinearDwTile::kBlocks)
   });
 }
 
-template <typename Tile, Major BM> int rows_as(unipool_ctx* ctx, int phase, const SimtLinear& p, cudaStream_t s) {
+template <typename Tile, Major BM, int S> int rows_as(unipool_ctx* ctx, int phase, const SimtLinear& p, cudaStream_t s) {
   PhaseTimer pt(ctx, phase, 1, s);
-  auto kern = linear_rows_kernel<Tile, BM>;
+  auto kern = linear_rows_kernel<Tile, BM, S>;
   constexpr int smem = (int)sizeof(typename Tile::Smem);
   UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  UP_KERNEL(kern, dim3((p.M + Tile::kRows - 1) / Tile::kRows, p.N / kSimtN), Tile::kThreads, smem, s, p);
+  UP_KERNEL(kern, dim3((p.M + Tile::kRows - 1) / Tile::kRows, p.N / kSimtN, S), Tile::kThreads, smem, s, p);
   return UNIPOOL_OK;
 }
 template <Major BM> int rows_simt(unipool_ctx* ctx, int phase, const SimtLinear& p, cudaStream_t s) {
   const int64_t tiles = (int64_t)((p.M + kSimtM - 1) / kSimtM) * (p.N / kSimtN);
-  if (tiles <= ctx->sm_count) return rows_as<SimtTile<8>, BM>(ctx, phase, p, s);
-  if (tiles <= 6 * ctx->sm_count) return rows_as<SimtTile<4>, BM>(ctx, phase, p, s);
-  return rows_as<SimtBlockTile<1>, BM>(ctx, phase, p, s);
+  // Tiles of four warps, three to an SM: as many to a tile as run at a time (a cluster of eight inside one GPC of 16 SMs), while each
+  // warp has two chunks.
+  const int chunks = p.K / kSimtKC;
+  auto fits = [&](int n) { return tiles * n <= (n == 8 ? 5 : 6) * ctx->sm_count / 2 && chunks >= 8 * n; };
+  if (2 * tiles <= ctx->sm_count) {
+    if (fits(8)) return rows_as<SimtTile<4>, BM, 8>(ctx, phase, p, s);
+    if (fits(4)) return rows_as<SimtTile<4>, BM, 4>(ctx, phase, p, s);
+    if (fits(2)) return rows_as<SimtTile<4>, BM, 2>(ctx, phase, p, s);
+  }
+  if (tiles <= ctx->sm_count) return rows_as<SimtTile<8>, BM, 1>(ctx, phase, p, s);
+  if (tiles <= 6 * ctx->sm_count) return rows_as<SimtTile<4>, BM, 1>(ctx, phase, p, s);
+  return rows_as<SimtBlockTile<1>, BM, 1>(ctx, phase, p, s);
 }
 
 // Parts of the tokens for the weight gradient: two blocks of tiles to an SM, 256 tokens at least to a part.
@@ -258,12 +303,7 @@ int dp_as(unipool_ctx* ctx, const LinearBwdArgs& a, int* blocks, float* parts, c
 }  // namespace
 
 int column_sum_launch(const float* parts, int n_parts, int64_t width, float* out, bool add, cudaStream_t s) {
-  // Few columns: every block's eight warps share the parts; many: each thread walks over them with 16-byte loads.
-  if (width % 4 == 0 && width >= 4 * 256 * 148 && aligned16(parts))
-    UP_KERNEL(part_sum_kernel, (unsigned)((width / 4 + 255) / 256), 256, 0, s, parts, n_parts, width, out, add);
-  else
-    UP_KERNEL(column_sum_kernel, (unsigned)((width + 7) / 8), 256, 0, s, parts, n_parts, width, out, add);
-  return UNIPOOL_OK;
+  return part_sum(PartSum{}, PartSum{parts, n_parts, width, out, add}, s);
 }
 
 int linear_launch(unipool_ctx* ctx, const LinearArgs& a, cudaStream_t s) {
@@ -284,7 +324,8 @@ static size_t dw_parts(const unipool_ctx* ctx, int T, int n_in, int n_out) {
 }
 size_t linear_bwd_scratch(const unipool_ctx* ctx, int T, int n_in, int n_out) {
   const int n = dp_row_blocks(ctx, T, n_out, 32 * (tensor_cores(ctx) ? 8 : 4)), m = dp_row_blocks(ctx, T, n_out, 32);
-  return (dw_parts(ctx, T, n_in, n_out) + (size_t)(n > m ? n : m) * n_out) * sizeof(float);
+  const size_t sums = n > m ? n : m;
+  return (dw_parts(ctx, T, n_in, n_out) + (sums > 1 ? sums * n_out : 0)) * sizeof(float);
 }
 
 int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) {
@@ -296,6 +337,7 @@ int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) 
   const bool tc = tensor_cores(ctx), act = a.act != UNIPOOL_ACT_NONE;
   const void* dp = act ? a.dp : a.dy;
   int rc = UNIPOOL_OK;
+  PartSum dW{}, db{};                                    // what is left to add up
   if (act || a.dbias != nullptr) {
     float* parts = a.scratch ? a.scratch + dw_parts(ctx, a.T, a.n_in, a.n_out) : nullptr;
     int blocks = 1;
@@ -303,11 +345,7 @@ int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) 
          : aligned16(a.dy, a.pre, act ? a.dp : nullptr) ? dp_as<float, 4, false>(ctx, a, &blocks, parts, s)
                                                         : dp_as<float, 1, false>(ctx, a, &blocks, parts, s);
     if (rc != UNIPOOL_OK) return rc;
-    if (a.dbias != nullptr && blocks > 1) {
-      PhaseTimer pt(ctx, UNIPOOL_PH_LINEAR_BWD, 1, s);
-      rc = column_sum_launch(parts, blocks, a.n_out, a.dbias, !a.overwrite, s);
-      if (rc != UNIPOOL_OK) return rc;
-    }
+    if (a.dbias != nullptr && blocks > 1) db = PartSum{parts, blocks, a.n_out, a.dbias, !a.overwrite};
   }
   if (a.dx != nullptr) {
     if (tc) {
@@ -322,14 +360,17 @@ int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) 
     }
     if (rc != UNIPOOL_OK) return rc;
   }
-  if (a.dW == nullptr) return UNIPOOL_OK;
-  const int splits = dw_splits(ctx, a.T, a.n_in, a.n_out);
-  float* out = splits > 1 ? a.scratch : a.dW;
-  const bool add = splits == 1 && !a.overwrite;
-  rc = tc ? linear_dw_tc(ctx, a, dp, out, splits, add, s) : dw_simt(ctx, a, dp, out, splits, add, s);
-  if (rc != UNIPOOL_OK || splits == 1) return rc;
+  if (a.dW != nullptr) {
+    const int splits = dw_splits(ctx, a.T, a.n_in, a.n_out);
+    float* out = splits > 1 ? a.scratch : a.dW;
+    const bool add = splits == 1 && !a.overwrite;
+    rc = tc ? linear_dw_tc(ctx, a, dp, out, splits, add, s) : dw_simt(ctx, a, dp, out, splits, add, s);
+    if (rc != UNIPOOL_OK) return rc;
+    if (splits > 1) dW = PartSum{a.scratch, splits, (int64_t)a.n_in * a.n_out, a.dW, !a.overwrite};
+  }
+  if (dW.n == 0 && db.n == 0) return UNIPOOL_OK;
   PhaseTimer pt(ctx, UNIPOOL_PH_LINEAR_BWD, 1, s);
-  return column_sum_launch(a.scratch, splits, (int64_t)a.n_in * a.n_out, a.dW, !a.overwrite, s);
+  return part_sum(dW, db, s);
 }
 
 }  // namespace unipool

@@ -42,6 +42,8 @@ template <int V> __device__ __forceinline__ void load_w(const float* w, float (&
 template <int V> __device__ __forceinline__ void store_e4m3(uint8_t* q, const float (&v)[V]) {
   if constexpr (V == 1) {
     *q = __nv_cvt_float_to_fp8(v[0], __NV_SATFINITE, __NV_E4M3);
+  } else if constexpr (V == 2) {
+    *reinterpret_cast<uint16_t*>(q) = __nv_cvt_float2_to_fp8x2(make_float2(v[0], v[1]), __NV_SATFINITE, __NV_E4M3);
   } else {
     uint32_t w[V / 4];
 #pragma unroll
@@ -55,8 +57,8 @@ template <int V> __device__ __forceinline__ void store_e4m3(uint8_t* q, const fl
   }
 }
 
-// The row's value of op over the TPR threads that share it, the same in all of them.  (TPR > 32: the block; `part` one
-// value per warp, not read by anyone any more.)
+// The row's value of op over the TPR threads that share it, the same in all of them: a warp, or the block (`part`: one value per warp,
+// not read by anyone any more).
 template <int TPR, typename F> __device__ __forceinline__ float row_reduce(float v, float* part, F op) {
 #pragma unroll
   for (int o = 16; o > 0; o >>= 1) v = op(v, __shfl_xor_sync(0xffffffffu, v, o));
@@ -169,6 +171,9 @@ struct NormBwdParams {
   int32_t* status;
 };
 
+// Bytes of the ring for a run of so many: it may begin and end inside 16 bytes.
+__host__ __device__ constexpr uint32_t norm_bwd_slot(uint32_t run) { return (run + 30) / 16 * 16; }
+
 // The sums over the warp of each of R values: the lane's own value of row row_of_lane<R>(lane) on return.  A lane hands half of its
 // values over at each step, until it has one.
 template <int R> __device__ __forceinline__ float reduce_rows(float (&v)[R], int lane) {
@@ -202,21 +207,21 @@ template <int R> __device__ __forceinline__ int row_of_lane(int lane) { return l
 // A block takes R rows at a time and a thread VPT vectors of the same columns of each: it keeps w and its sums for dw in
 // registers over all its rows, and the rows' dot products cost one barrier for R of them.  (With a row to a warp the sums of a whole
 // row lay in every warp's registers, and they had to be added up at the end: 16384 rows of 768 bf16 22.5 us instead of 19.5, and more to add up behind it.)
-// kRing: R rows are one run of bytes in memory, a multiple of 16 of them; runs are copied into a ring in shared memory some
-// stages ahead, so that reads go on while rows are worked on and whatever the rows' alignment (16384 rows of 770 bf16 read
+// kRing: R rows are one run of bytes in memory; runs are copied, from the 16-byte boundary below to the one above, into a ring in
+// shared memory some stages ahead, so that reads go on while rows are worked on and whatever the rows' alignment (16384 rows of 770 bf16 read
 // element by element 69 us, through the ring 37).  Without it (arrays off 16 bytes, rows too long for two stages) the loads go
 // from memory into registers.
 // The sums' order depends on the sizes alone.
 template <typename E, int V, int VPT, int R, bool kRing>
-__global__ void __launch_bounds__(512) rmsnorm_bwd_kernel(NormBwdParams p) {
+__global__ void __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_kernel(NormBwdParams p) {
   extern __shared__ __align__(128) uint8_t ring[];       // [stages][dh, r, dr][R rows], then the barriers
   __shared__ float part[2][16][R];
   __shared__ int abort_word;
   constexpr bool kKeepW = VPT * V <= 16;                 // else w comes from the cache again
   const int t = threadIdx.x, n_warps = blockDim.x / 32;
-  const uint32_t run = (uint32_t)(R * p.width * (int)sizeof(E));
+  const uint32_t run = (uint32_t)(R * p.width * (int)sizeof(E)), slot = norm_bwd_slot(run);
   const int arrays = p.dr != nullptr ? 3 : 2;
-  uint64_t* full = reinterpret_cast<uint64_t*>(ring + (size_t)p.stages * arrays * run);
+  uint64_t* full = reinterpret_cast<uint64_t*>(ring + (size_t)p.stages * arrays * slot);
   volatile int* abort = &abort_word;
   if constexpr (kRing) {
     if (t == 0) {
@@ -228,17 +233,18 @@ __global__ void __launch_bounds__(512) rmsnorm_bwd_kernel(NormBwdParams p) {
   }
   grid_wait(p.dh, p.r, p.dr, p.w, p.rstd);
   const int64_t groups = ((int64_t)p.T + R - 1) / R;
-  // Rows of group g into its stage: by the copy engine, if they end on 16 bytes (the last ones may not).
-  auto bytes_of = [&](int64_t g) { return (uint32_t)(min((int64_t)R, p.T - g * R) * p.width * (int)sizeof(E)); };
+  // Rows of group g into its stage: by the copy engine, but for the last ones, where that would reach beyond the array's end.
+  const int64_t total = (int64_t)p.T * p.width * (int)sizeof(E);
+  auto end_of = [&](int64_t g) { return (min((g + 1) * (int64_t)run, total) + 15) / 16 * 16; };
   auto fetch = [&](int64_t g, int stage) {
-    const uint32_t n = bytes_of(g);
-    if (n % 16 != 0) return;
-    uint8_t* to = ring + (size_t)stage * arrays * run;
-    const int64_t from = g * run;
+    const int64_t from = g * run / 16 * 16;
+    if (end_of(g) > total) return;
+    const uint32_t n = (uint32_t)(end_of(g) - from);
+    uint8_t* to = ring + (size_t)stage * arrays * slot;
     tc::mbar_expect_tx(&full[stage], arrays * n);
     tc::bulk_load(to, static_cast<const uint8_t*>(p.dh) + from, n, &full[stage]);
-    tc::bulk_load(to + run, static_cast<const uint8_t*>(p.r) + from, n, &full[stage]);
-    if (arrays == 3) tc::bulk_load(to + 2 * run, static_cast<const uint8_t*>(p.dr) + from, n, &full[stage]);
+    tc::bulk_load(to + slot, static_cast<const uint8_t*>(p.r) + from, n, &full[stage]);
+    if (arrays == 3) tc::bulk_load(to + 2 * slot, static_cast<const uint8_t*>(p.dr) + from, n, &full[stage]);
   };
   if (kRing && t == 0) {
     int64_t g = blockIdx.x;
@@ -266,9 +272,9 @@ __global__ void __launch_bounds__(512) rmsnorm_bwd_kernel(NormBwdParams p) {
   load_rstd(blockIdx.x);
   for (int64_t g = blockIdx.x; g < groups; g += gridDim.x, turn ^= 1) {
     const int64_t row0 = g * R;
-    const uint8_t* at_stage = ring + (size_t)stage * arrays * run;
+    uint8_t* at_stage = ring + (size_t)stage * arrays * slot + g * run % 16;
     if constexpr (kRing) {
-      if (bytes_of(g) % 16 == 0) {
+      if (end_of(g) <= total) {
         // (a wait that runs out is reported, and no later one waits; the block goes on to its end)
         if (!*abort && !tc::mbar_wait(&full[stage], phase, abort)) {
           *abort = 1;
@@ -276,11 +282,11 @@ __global__ void __launch_bounds__(512) rmsnorm_bwd_kernel(NormBwdParams p) {
         }
       } else {
         const int64_t from = row0 * p.width;
-        for (int c = t; c < (int)(p.T - row0) * p.width; c += blockDim.x) {
-          E* to = reinterpret_cast<E*>(ring + (size_t)stage * arrays * run) + c;
-          to[0] = static_cast<const E*>(p.dh)[from + c];
-          to[R * p.width] = static_cast<const E*>(p.r)[from + c];
-          if (arrays == 3) to[2 * R * p.width] = static_cast<const E*>(p.dr)[from + c];
+        const int n = (int)min((int64_t)R, p.T - row0) * p.width;
+        for (int c = t; c < n; c += blockDim.x) {
+          reinterpret_cast<E*>(at_stage)[c] = static_cast<const E*>(p.dh)[from + c];
+          reinterpret_cast<E*>(at_stage + slot)[c] = static_cast<const E*>(p.r)[from + c];
+          if (arrays == 3) reinterpret_cast<E*>(at_stage + 2 * slot)[c] = static_cast<const E*>(p.dr)[from + c];
         }
         __syncthreads();
       }
@@ -299,8 +305,8 @@ __global__ void __launch_bounds__(512) rmsnorm_bwd_kernel(NormBwdParams p) {
           const E *x, *y, *z;
           if constexpr (kRing) {
             x = reinterpret_cast<const E*>(at_stage) + (k * p.width + c);
-            y = x + R * p.width;
-            z = y + R * p.width;
+            y = reinterpret_cast<const E*>(at_stage + slot) + (k * p.width + c);
+            z = reinterpret_cast<const E*>(at_stage + 2 * slot) + (k * p.width + c);
           } else {
             const int64_t at = (row0 + k) * p.width + c;
             x = static_cast<const E*>(p.dh) + at;
@@ -406,8 +412,8 @@ __global__ void __launch_bounds__(512) rmsnorm_bwd_kernel(NormBwdParams p) {
 // How the backward kernel runs: elements of a vector, vectors of a thread, threads and rows of a block, blocks, stages of the ring
 // (0: none) and its bytes.
 struct NormBwdShape { int v, vpt, threads, rows, blocks, stages; uint32_t smem; };
-constexpr int norm_bwd_rows(int V, int bytes, int vpt) {   // 24 to 48 registers of elements; 16 bytes of a column where they fit
-  return V * bytes == 16 ? (vpt >= 4 ? 1 : 4 / vpt) : (vpt >= 16 ? 1 : vpt == 8 ? 2 : vpt == 4 || bytes == 4 ? 4 : 8);
+constexpr int norm_bwd_rows(int V, int bytes, int vpt) {   // 48 registers of elements, 24 of narrower vectors
+  return V * bytes == 16 ? (vpt >= 4 ? 1 : 4 / vpt) : vpt >= 8 ? 1 : 8 / (vpt * (V * bytes == 8 ? 2 : 1));
 }
 NormBwdShape norm_bwd_shape_of(const unipool_ctx* ctx, int T, int width, int v, bool aligned, int arrays) {
   const int e = (int)ctx->elem_bytes, n = (width + v - 1) / v;
@@ -416,18 +422,20 @@ NormBwdShape norm_bwd_shape_of(const unipool_ctx* ctx, int T, int width, int v, 
   s.vpt = n <= 512 ? 1 : n <= 1024 ? 2 : n <= 2048 ? 4 : n <= 4096 ? 8 : 32;
   s.threads = ((n + s.vpt - 1) / s.vpt + 31) / 32 * 32;
   s.rows = norm_bwd_rows(v, e, s.vpt);
-  const int64_t stage = (int64_t)s.rows * width * e * arrays;
-  int per_sm = s.threads <= 320 ? 640 / s.threads : 1;
+  const int64_t stage = (int64_t)norm_bwd_slot((uint32_t)(s.rows * width * e)) * arrays;
+  const int threads = v * e == 16 ? 640 : 1024;          // on an SM, by their registers
+  int per_sm = 2 * s.threads <= threads ? threads / s.threads : 1;
   per_sm = per_sm > 16 ? 16 : per_sm;
   s.stages = 0;
-  if (aligned && (int64_t)s.rows * width * e % 16 == 0 && s.vpt <= 8) {
+  if (aligned && s.vpt <= 8) {
     auto fit = [&](int blocks) { return (int)((220 * 1024 / blocks - 2304) / stage); };     // (2304: barriers, sums, the system's)
     while (per_sm > 1 && fit(per_sm) < 2) --per_sm;
     s.stages = fit(per_sm) > 4 ? 4 : fit(per_sm) < 2 ? 0 : fit(per_sm);
   }
   s.smem = s.stages > 0 ? (uint32_t)(s.stages * stage + 64) : 0;
+  // (few rows on one block: no sums to add up behind it, which costs as much as three steps of a block)
   const int all = (T + s.rows - 1) / s.rows, most = ctx->sm_count * per_sm;
-  s.blocks = all < most ? all : most;
+  s.blocks = all <= 4 ? 1 : all < most ? all : most;
   return s;
 }
 NormBwdShape norm_bwd_shape(const unipool_ctx* ctx, int T, int width, bool aligned, int arrays) {
@@ -440,45 +448,44 @@ NormBwdShape norm_bwd_shape(const unipool_ctx* ctx, int T, int width, bool align
   return norm_bwd_shape_of(ctx, T, width, 1, aligned, arrays);
 }
 
-// Calls f(TPR, VPT) as compile-time numbers for rows of `n` vectors.
 template <int N> using Int = std::integral_constant<int, N>;
-template <bool kScalar, typename F> int by_width(int n, F f) {
-  if constexpr (!kScalar) {
-    if (n <= 32) return f(Int<32>(), Int<1>());
-    if (n <= 64) return f(Int<32>(), Int<2>());
-    if (n <= 96) return f(Int<32>(), Int<3>());
-    if (n <= 128) return f(Int<32>(), Int<4>());
-    if (n <= 192) return f(Int<32>(), Int<6>());
-    if (n <= 256) return f(Int<32>(), Int<8>());
-    if (n <= 512) return f(Int<128>(), Int<4>());
-    if (n <= 1024) return f(Int<128>(), Int<8>());
-    if (n <= 2048) return f(Int<512>(), Int<4>());
-    return f(Int<512>(), Int<8>());
-  } else {
-    if (n <= 256) return f(Int<32>(), Int<8>());
-    if (n <= 1024) return f(Int<128>(), Int<8>());
-    if (n <= 4096) return f(Int<512>(), Int<8>());
-    return f(Int<512>(), Int<32>());
-  }
-}
-
-// Calls f(E, V, TPR, VPT) for the element type and what of the rows fits 16-byte accesses.
-template <typename E, typename F> int by_row(bool vec, int width, F f) {
-  constexpr int V = 16 / (int)sizeof(E);
-  if (vec) return by_width<false>(width / V, [&](auto tpr, auto vpt) { return f(E(), Int<V>(), tpr, vpt); });
-  return by_width<true>(width, [&](auto tpr, auto vpt) { return f(E(), Int<1>(), tpr, vpt); });
-}
 
 template <bool kNorm, typename E> int norm_as(unipool_ctx* ctx, const NormParams& p, cudaStream_t s) {
+  constexpr int V = 16 / (int)sizeof(E);
   const uintptr_t rows = reinterpret_cast<uintptr_t>(p.x) | reinterpret_cast<uintptr_t>(p.y) | reinterpret_cast<uintptr_t>(p.r) |
                          reinterpret_cast<uintptr_t>(p.h) | reinterpret_cast<uintptr_t>(p.w);
-  const bool vec = (int64_t)p.width * sizeof(E) % 16 == 0 && rows % 16 == 0 && reinterpret_cast<uintptr_t>(p.q) % 8 == 0;
-  return by_row<E>(vec, p.width, [&](auto e, auto v, auto tpr, auto vpt) {
-    constexpr int kRows = kNormThreads<tpr> / tpr;
+  auto run = [&](auto v, auto tpr, auto vpt) {
+    constexpr int kTpr = decltype(tpr)::value, kRows = kNormThreads<kTpr> / kTpr;
     PhaseTimer pt(ctx, UNIPOOL_PH_RMSNORM, 1, s);
-    UP_KERNEL((rmsnorm_kernel<decltype(e), v, tpr, vpt, kNorm>), (p.T + kRows - 1) / kRows, kNormThreads<tpr>, 0, s, p);
+    UP_KERNEL((rmsnorm_kernel<E, decltype(v)::value, kTpr, decltype(vpt)::value, kNorm>), (p.T + kRows - 1) / kRows, kNormThreads<kTpr>,
+              0, s, p);
     return UNIPOOL_OK;
-  });
+  };
+  // vectors of v elements whose number and rows' alignment allow them
+  auto fits = [&](int v) { return p.width % v == 0 && rows % (v * sizeof(E)) == 0 && rows % (v * 4 < 16 ? v * 4 : 16) == 0 &&
+                                  reinterpret_cast<uintptr_t>(p.q) % v == 0; };
+  if (fits(V)) {
+    const int n = p.width / V;
+    if (n <= 32) return run(Int<V>(), Int<32>(), Int<1>());
+    if (n <= 64) return run(Int<V>(), Int<32>(), Int<2>());
+    if (n <= 96) return run(Int<V>(), Int<32>(), Int<3>());
+    if (n <= 128) return run(Int<V>(), Int<32>(), Int<4>());
+    if (n <= 192) return run(Int<V>(), Int<32>(), Int<6>());
+    if (n <= 256) return run(Int<V>(), Int<32>(), Int<8>());
+    if (n <= 512) return run(Int<V>(), Int<128>(), Int<4>());
+    if (n <= 1024) return run(Int<V>(), Int<256>(), Int<4>());
+    return n <= 2048 ? run(Int<V>(), Int<512>(), Int<4>()) : run(Int<V>(), Int<512>(), Int<8>());
+  }
+  auto narrow = [&](auto v) {
+    const int n = p.width / decltype(v)::value;
+    if (n <= 256) return run(v, Int<32>(), Int<8>());
+    if (n <= 1024) return run(v, Int<128>(), Int<8>());
+    if (n <= 2048) return run(v, Int<256>(), Int<8>());
+    if (n <= 2560) return run(v, Int<320>(), Int<8>());
+    if (n <= 4096) return run(v, Int<512>(), Int<8>());
+    return run(v, Int<512>(), Int<32>());
+  };
+  return fits(2) ? narrow(Int<2>()) : narrow(Int<1>());
 }
 
 template <typename E, int V, int VPT, bool kRing>
@@ -527,7 +534,7 @@ size_t rmsnorm_bwd_scratch(const unipool_ctx* ctx, int T, int width) {
     const int n = norm_bwd_shape(ctx, T, width, (k & 1) != 0, k < 2 ? 2 : 3).blocks;
     most = n > most ? n : most;
   }
-  return (size_t)most * width * sizeof(float);
+  return most > 1 ? (size_t)most * width * sizeof(float) : 0;
 }
 
 int rmsnorm_launch(unipool_ctx* ctx, const void* x, const void* y, int T, int width, const float* w, float eps, void* r,
