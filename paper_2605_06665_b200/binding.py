@@ -226,6 +226,7 @@ class Context:
         _check(lib().unipool_create(ctypes.byref(self.handle), ctypes.byref(cfg), _p(self.workspace),
                                     self.workspace.numel(), _stream()))
         self.row_capacity = row_capacity(cfg)
+        self._sizes = {}                                   # scratch sizes that were asked for
 
     def close(self):
         if self.handle:
@@ -331,11 +332,18 @@ class Context:
 
     def rmsnorm_bwd_scratch(self, T, width):
         """Bytes that rmsnorm_bwd needs beside its results."""
-        return lib().unipool_rmsnorm_bwd_scratch(self.handle, T, width)
+        return self._size(lib().unipool_rmsnorm_bwd_scratch, T, width)
 
     def linear_bwd_scratch(self, T, n_in, n_out):
         """Bytes that linear_bwd needs beside its results."""
-        return lib().unipool_linear_bwd_scratch(self.handle, T, n_in, n_out)
+        return self._size(lib().unipool_linear_bwd_scratch, T, n_in, n_out)
+
+    def _size(self, f, *shape):
+        if shape not in self._sizes:                       # (two numbers or three: the norm's and the product's are apart)
+            if len(self._sizes) > 1000:
+                self._sizes.clear()
+            self._sizes[shape] = f(self.handle, *shape)
+        return self._sizes[shape]
 
     def _scratch(self, nbytes):
         """Device memory for one call: the allocator hands it on to later work of the same stream only."""

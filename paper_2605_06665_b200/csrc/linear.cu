@@ -93,12 +93,13 @@ int dp_row_blocks(const unipool_ctx* ctx, int T, int N, int cols_per_block) {
 }
 
 // ---------------------------------------------------------------- sums of parts, in their order
-// out [width] (+)= the sum over n parts [n, width].
-struct PartSum { const float* parts; int n; int64_t width; float* out; bool add; };
+// out [width] (+)= the sum over n parts [n, width] of type P.
+template <typename P> struct PartSum { const P* parts; int n; int64_t width; float* out; bool add; };
 
 // Blocks [0, wide_blocks): few parts of many columns (a weight gradient's), four columns to a thread, 16 bytes at a time.  The others:
-// many parts of few columns, eight columns, a sector, to a block, whose 32 groups of eight threads take every 32nd part.
-__global__ void __launch_bounds__(256) part_sum_kernel(PartSum wide, int wide_blocks, PartSum tall) {
+// many parts of few columns, a sector of them to a block, whose 32 groups of eight threads take every 32nd part.
+template <typename P>
+__global__ void __launch_bounds__(256) part_sum_kernel(PartSum<float> wide, int wide_blocks, PartSum<P> tall) {
   grid_wait(wide.parts, tall.parts);
   if ((int)blockIdx.x < wide_blocks) {
     const int64_t c = ((int64_t)blockIdx.x * 256 + threadIdx.x) * 4;
@@ -114,27 +115,42 @@ __global__ void __launch_bounds__(256) part_sum_kernel(PartSum wide, int wide_bl
     st4(out, v, (reinterpret_cast<uintptr_t>(out) & 15) == 0);
     return;
   }
-  __shared__ float s[8][8];
+  constexpr int V = 4 / (int)sizeof(P);                  // columns of a thread
+  __shared__ float s[8][8 * V];
   const int lane = threadIdx.x % 32, g = threadIdx.x / 8;
-  const int64_t c = (int64_t)(blockIdx.x - wide_blocks) * 8 + threadIdx.x % 8;
-  float v = 0.f;
+  const int64_t c = ((int64_t)(blockIdx.x - wide_blocks) * 8 + threadIdx.x % 8) * V;
+  float v[V];
+#pragma unroll
+  for (int j = 0; j < V; ++j) v[j] = 0.f;
   if (c < tall.width) {
 #pragma unroll 8
-    for (int i = g; i < tall.n; i += 32) v += __ldg(tall.parts + i * tall.width + c);
-  }
-  v += __shfl_xor_sync(0xffffffffu, v, 8);
-  v += __shfl_xor_sync(0xffffffffu, v, 16);
-  if (lane < 8) s[threadIdx.x / 32][lane] = v;
-  __syncthreads();
-  if (threadIdx.x >= 8 || c >= tall.width) return;
-  v = s[0][lane];
+    for (int i = g; i < tall.n; i += 32) {
+      Vec<P, V> r;
+      float u[V];
+      r.load(tall.parts + i * tall.width + c);
+      r.get(u);
 #pragma unroll
-  for (int i = 1; i < 8; ++i) v += s[i][lane];
-  tall.out[c] = tall.add ? tall.out[c] + v : v;
+      for (int j = 0; j < V; ++j) v[j] += u[j];
+    }
+  }
+#pragma unroll
+  for (int j = 0; j < V; ++j) {
+    v[j] += __shfl_xor_sync(0xffffffffu, v[j], 8);
+    v[j] += __shfl_xor_sync(0xffffffffu, v[j], 16);
+    if (lane < 8) s[threadIdx.x / 32][lane * V + j] = v[j];
+  }
+  __syncthreads();
+  const int64_t col = (int64_t)(blockIdx.x - wide_blocks) * 8 * V + threadIdx.x;
+  if (threadIdx.x >= 8 * V || col >= tall.width) return;
+  float sum = s[0][threadIdx.x];
+#pragma unroll
+  for (int i = 1; i < 8; ++i) sum += s[i][threadIdx.x];
+  tall.out[col] = tall.add ? tall.out[col] + sum : sum;
 }
-int part_sum(const PartSum& wide, const PartSum& tall, cudaStream_t s) {       // (one of n = 0: none)
-  const int a = wide.n > 0 ? (int)((wide.width / 4 + 255) / 256) : 0, b = tall.n > 0 ? (int)((tall.width + 7) / 8) : 0;
-  if (a + b > 0) UP_KERNEL(part_sum_kernel, a + b, 256, 0, s, wide, a, tall);
+template <typename P> int part_sum(const PartSum<float>& wide, const PartSum<P>& tall, cudaStream_t s) {   // (one of n = 0: none)
+  constexpr int kCols = 8 * 4 / (int)sizeof(P);
+  const int a = wide.n > 0 ? (int)((wide.width / 4 + 255) / 256) : 0, b = tall.n > 0 ? (int)((tall.width + kCols - 1) / kCols) : 0;
+  if (a + b > 0) UP_KERNEL(part_sum_kernel<P>, a + b, 256, 0, s, wide, a, tall);
   return UNIPOOL_OK;
 }
 
@@ -281,6 +297,8 @@ int dw_simt(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, float* out
   return UNIPOOL_OK;
 }
 
+constexpr int kDyRows = 512;             // so few rows of dy are summed without a kernel of their own
+
 bool tensor_cores(const unipool_ctx* ctx) { return ctx->cfg.dtype == UNIPOOL_BF16; }
 int dw_splits(const unipool_ctx* ctx, int T, int n_in, int n_out) {
   return tensor_cores(ctx) ? linear_dw_splits_tc(ctx, T, n_in, n_out) : dw_splits_simt(ctx, T, n_in, n_out);
@@ -303,7 +321,7 @@ int dp_as(unipool_ctx* ctx, const LinearBwdArgs& a, int* blocks, float* parts, c
 }  // namespace
 
 int column_sum_launch(const float* parts, int n_parts, int64_t width, float* out, bool add, cudaStream_t s) {
-  return part_sum(PartSum{}, PartSum{parts, n_parts, width, out, add}, s);
+  return part_sum(PartSum<float>{}, PartSum<float>{parts, n_parts, width, out, add}, s);
 }
 
 int linear_launch(unipool_ctx* ctx, const LinearArgs& a, cudaStream_t s) {
@@ -337,15 +355,17 @@ int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) 
   const bool tc = tensor_cores(ctx), act = a.act != UNIPOOL_ACT_NONE;
   const void* dp = act ? a.dp : a.dy;
   int rc = UNIPOOL_OK;
-  PartSum dW{}, db{};                                    // what is left to add up
-  if (act || a.dbias != nullptr) {
+  PartSum<float> dW{}, db{};                             // what is left to add up
+  // (few rows of dy itself are added up beside dW's parts: one launch less)
+  const bool dy_rows = !act && a.dbias != nullptr && a.T <= kDyRows;
+  if (act || (a.dbias != nullptr && !dy_rows)) {
     float* parts = a.scratch ? a.scratch + dw_parts(ctx, a.T, a.n_in, a.n_out) : nullptr;
     int blocks = 1;
     rc = tc ? dp_as<__nv_bfloat16, 8, true>(ctx, a, &blocks, parts, s)
          : aligned16(a.dy, a.pre, act ? a.dp : nullptr) ? dp_as<float, 4, false>(ctx, a, &blocks, parts, s)
                                                         : dp_as<float, 1, false>(ctx, a, &blocks, parts, s);
     if (rc != UNIPOOL_OK) return rc;
-    if (a.dbias != nullptr && blocks > 1) db = PartSum{parts, blocks, a.n_out, a.dbias, !a.overwrite};
+    if (a.dbias != nullptr && blocks > 1) db = {parts, blocks, a.n_out, a.dbias, !a.overwrite};
   }
   if (a.dx != nullptr) {
     if (tc) {
@@ -366,11 +386,13 @@ int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) 
     const bool add = splits == 1 && !a.overwrite;
     rc = tc ? linear_dw_tc(ctx, a, dp, out, splits, add, s) : dw_simt(ctx, a, dp, out, splits, add, s);
     if (rc != UNIPOOL_OK) return rc;
-    if (splits > 1) dW = PartSum{a.scratch, splits, (int64_t)a.n_in * a.n_out, a.dW, !a.overwrite};
+    if (splits > 1) dW = {a.scratch, splits, (int64_t)a.n_in * a.n_out, a.dW, !a.overwrite};
   }
-  if (dW.n == 0 && db.n == 0) return UNIPOOL_OK;
+  if (dW.n == 0 && db.n == 0 && !dy_rows) return UNIPOOL_OK;
   PhaseTimer pt(ctx, UNIPOOL_PH_LINEAR_BWD, 1, s);
-  return part_sum(dW, db, s);
+  if (!dy_rows) return part_sum(dW, db, s);
+  if (tc) return part_sum(dW, PartSum<__nv_bfloat16>{static_cast<const __nv_bfloat16*>(a.dy), a.T, a.n_out, a.dbias, !a.overwrite}, s);
+  return part_sum(dW, PartSum<float>{static_cast<const float*>(a.dy), a.T, a.n_out, a.dbias, !a.overwrite}, s);
 }
 
 }  // namespace unipool
