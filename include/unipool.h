@@ -362,16 +362,17 @@ int unipool_stack_backward(unipool_ctx* ctx, const unipool_stack* stack, int32_t
  *   r = x + y;  n_t = 1 / sqrt(mean_j r_tj^2 + eps);  h = r * n_t * w;
  *   q = e4m3(h / s_t) with s_t = max(max_j |h_tj| / 448, 2^-126), rounded to nearest even.
  * The statistics are fp32 and h is formed from the unrounded sum; each output is rounded once.  A row that holds
- * a NaN has NaN in rstd, h, q and q_scale; infinities follow the formulas.
+ * a NaN has NaN in rstd, h, q and q_scale; infinities follow the formulas, as do sums of squares that pass fp32's
+ * range (rstd 0).  With eps = 0 a row of zeros has no norm (NaN).
  * in : x [T,width] (ctx dtype); y [T,width] or NULL (r = x); w [width] float; eps >= 0.
  * out: r [T,width] (ctx dtype) or NULL; rstd [T] float (n_t, kept for the backward call) or NULL; h [T,width]
  *      (ctx dtype) or NULL; q [T,width] e4m3 (one byte each) and q_scale [T] float, or both NULL; h or q is given.
- *      r and h may each be x or y. */
+ *      r and h may each be x or y; q lies apart from all of them. */
 int unipool_rmsnorm(unipool_ctx* ctx, const void* x, const void* y, int32_t T, int32_t width, const float* w, float eps,
                     void* r, float* rstd, void* h, uint8_t* q, float* q_scale, unipool_stream stream);
 
-/* Backward of unipool_rmsnorm.  With c_t = sum_j dh_tj w_j r_tj:
- *   dx = rstd w dh - r rstd^3 c / width (+ dr),   dw_j += sum_t dh_tj rstd_t r_tj
+/* Backward of unipool_rmsnorm.  With xhat_tj = r_tj rstd_t:
+ *   dx = rstd (w dh - xhat mean_j(w dh xhat)) (+ dr),   dw_j += sum_t dh_tj xhat_tj
  * (dx is the gradient of x and of y alike; dr that of r itself, which the residual stream brings).
  * in : dh [T,width]; r [T,width] as the forward call stored it (its x where it had no y); w; rstd; dr [T,width] or
  *      NULL; scratch: unipool_rmsnorm_bwd_scratch() bytes of device memory, 16-byte aligned, which the call may

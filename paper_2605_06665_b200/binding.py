@@ -174,6 +174,15 @@ def _p(t):
     return None if t is None else t.data_ptr()
 
 
+def _d(t):
+    """The same of a tensor that has to be dense."""
+    if t is None:
+        return None
+    if not t.is_contiguous():
+        raise ValueError(f"a tensor of shape {tuple(t.shape)} and strides {t.stride()} is not dense row-major")
+    return t.data_ptr()
+
+
 _raw_stream = None
 
 
@@ -301,34 +310,34 @@ class Context:
 
     # ---- the operators around the MoE layer
     def rmsnorm(self, x, y, T, width, w, eps, r, rstd, h, q=None, q_scale=None):
-        _check(lib().unipool_rmsnorm(self.handle, _p(x), _p(y), T, width, _p(w), eps, _p(r), _p(rstd), _p(h), _p(q),
-                                     _p(q_scale), _stream()))
+        _check(lib().unipool_rmsnorm(self.handle, _d(x), _d(y), T, width, _d(w), eps, _d(r), _d(rstd), _d(h), _d(q),
+                                     _d(q_scale), _stream()))
 
     def rmsnorm_bwd(self, dh, r, T, width, w, rstd, dr, dx, dw, flags=0, scratch=None):
         """``scratch``: a device tensor of unipool_rmsnorm_bwd_scratch() bytes; allocated per call if None."""
-        if scratch is None and dw is not None:
-            scratch = self._scratch(self.rmsnorm_bwd_scratch(T, width))
-        _check(lib().unipool_rmsnorm_bwd(self.handle, _p(dh), _p(r), T, width, _p(w), _p(rstd), _p(dr), _p(dx), _p(dw),
-                                         _p(scratch), flags, _stream()))
+        if dw is not None:
+            scratch = self._scratch(self.rmsnorm_bwd_scratch(T, width), scratch)
+        _check(lib().unipool_rmsnorm_bwd(self.handle, _d(dh), _d(r), T, width, _d(w), _d(rstd), _d(dr), _d(dx), _d(dw),
+                                         _d(scratch), flags, _stream()))
 
     def quantize_rows(self, x, rows, width, q, q_scale):
-        _check(lib().unipool_quantize_rows(self.handle, _p(x), rows, width, _p(q), _p(q_scale), _stream()))
+        _check(lib().unipool_quantize_rows(self.handle, _d(x), rows, width, _d(q), _d(q_scale), _stream()))
 
     def linear(self, x, T, n_in, W, n_out, bias, act, residual, pre, y):
         """``act``: a value of ACTIVATIONS."""
-        _check(lib().unipool_linear(self.handle, _p(x), T, n_in, _p(W), n_out, _p(bias), act, _p(residual), _p(pre), _p(y),
+        _check(lib().unipool_linear(self.handle, _d(x), T, n_in, _d(W), n_out, _d(bias), act, _d(residual), _d(pre), _d(y),
                                     _stream()))
 
     def linear_scaled(self, x, x_scale, T, n_in, W, w_scale, n_out, bias, act, residual, pre, y):
-        _check(lib().unipool_linear_scaled(self.handle, _p(x), _p(x_scale), T, n_in, _p(W), _p(w_scale), n_out, _p(bias),
-                                           act, _p(residual), _p(pre), _p(y), _stream()))
+        _check(lib().unipool_linear_scaled(self.handle, _d(x), _d(x_scale), T, n_in, _d(W), _d(w_scale), n_out, _d(bias),
+                                           act, _d(residual), _d(pre), _d(y), _stream()))
 
     def linear_bwd(self, dy, T, n_out, pre, act, x, n_in, W, dp, dx_residual, dx, dW, dbias, flags=0, scratch=None):
         """``scratch``: a device tensor of unipool_linear_bwd_scratch() bytes; allocated per call if None."""
-        if scratch is None and (dW is not None or dbias is not None):
-            scratch = self._scratch(self.linear_bwd_scratch(T, n_in, n_out))
-        _check(lib().unipool_linear_bwd(self.handle, _p(dy), T, n_out, _p(pre), act, _p(x), n_in, _p(W), _p(dp),
-                                        _p(dx_residual), _p(dx), _p(dW), _p(dbias), _p(scratch), flags, _stream()))
+        if dW is not None or dbias is not None:
+            scratch = self._scratch(self.linear_bwd_scratch(T, n_in, n_out), scratch)
+        _check(lib().unipool_linear_bwd(self.handle, _d(dy), T, n_out, _d(pre), act, _d(x), n_in, _d(W), _d(dp),
+                                        _d(dx_residual), _d(dx), _d(dW), _d(dbias), _d(scratch), flags, _stream()))
 
     def rmsnorm_bwd_scratch(self, T, width):
         """Bytes that rmsnorm_bwd needs beside its results."""
@@ -345,8 +354,13 @@ class Context:
             self._sizes[shape] = f(self.handle, *shape)
         return self._sizes[shape]
 
-    def _scratch(self, nbytes):
-        """Device memory for one call: the allocator hands it on to later work of the same stream only."""
+    def _scratch(self, nbytes, given):
+        """Device memory for one call: what the caller gave, or new (the allocator hands it on to later work of the same
+        stream only)."""
+        if given is not None:
+            if given.numel() * given.element_size() < nbytes:
+                raise ValueError(f"scratch of {given.numel() * given.element_size()} bytes, {nbytes} needed")
+            return given
         import torch
         return torch.empty(nbytes, dtype=torch.uint8, device=self.device) if nbytes else None
 

@@ -114,6 +114,14 @@ static int validate_config(const unipool_config* c) {
 using namespace unipool;
 
 #define CHECK_CTX(ctx) UP_REQUIRE((ctx) != nullptr, UNIPOOL_ERR_INVALID_ARG, "ctx is NULL")
+// A stream and pointers of the context's device are nothing to another one.
+#define CHECK_DEVICE(ctx)                                                                                              \
+  do {                                                                                                                 \
+    int device__ = (ctx)->device;                                                                                      \
+    UP_CUDA(cudaGetDevice(&device__));                                                                                 \
+    UP_REQUIRE(device__ == (ctx)->device, UNIPOOL_ERR_INVALID_ARG, "a context of device %d, while device %d is current", \
+               (ctx)->device, device__);                                                                               \
+  } while (0)
 #define CHECK_PTR(p) UP_REQUIRE((p) != nullptr, UNIPOOL_ERR_INVALID_ARG, #p " is NULL")
 #define CHECK_SCRATCH(p)                                                             \
   UP_REQUIRE((p) != nullptr && (reinterpret_cast<uintptr_t>(p) & 15) == 0,           \
@@ -413,7 +421,7 @@ int unipool_route_bwd(unipool_ctx* ctx, const void* x, int32_t T, const float* W
 
 int unipool_rmsnorm(unipool_ctx* ctx, const void* x, const void* y, int32_t T, int32_t width, const float* w, float eps,
                     void* r, float* rstd, void* h, uint8_t* q, float* q_scale, unipool_stream stream) {
-  CHECK_CTX(ctx); CHECK_T(ctx, T); CHECK_WIDTH(width);
+  CHECK_CTX(ctx); CHECK_DEVICE(ctx); CHECK_T(ctx, T); CHECK_WIDTH(width);
   CHECK_PTR(x); CHECK_PTR(w);
   UP_REQUIRE(eps >= 0.f, UNIPOOL_ERR_INVALID_ARG, "eps must be >= 0");
   UP_REQUIRE(h != nullptr || q != nullptr, UNIPOOL_ERR_INVALID_ARG, "h and q are both NULL");
@@ -429,7 +437,7 @@ size_t unipool_rmsnorm_bwd_scratch(const unipool_ctx* ctx, int32_t T, int32_t wi
 int unipool_rmsnorm_bwd(unipool_ctx* ctx, const void* dh, const void* r, int32_t T, int32_t width, const float* w,
                         const float* rstd, const void* dr, void* dx, float* dw, void* scratch, int32_t flags,
                         unipool_stream stream) {
-  CHECK_CTX(ctx); CHECK_T(ctx, T); CHECK_WIDTH(width);
+  CHECK_CTX(ctx); CHECK_DEVICE(ctx); CHECK_T(ctx, T); CHECK_WIDTH(width);
   CHECK_PTR(dh); CHECK_PTR(r); CHECK_PTR(w); CHECK_PTR(rstd); CHECK_PTR(dx);
   UP_REQUIRE((flags & ~UNIPOOL_WGRAD_OVERWRITE) == 0, UNIPOOL_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
   if (dw != nullptr && T > 0 && rmsnorm_bwd_scratch(ctx, T, width) > 0) CHECK_SCRATCH(scratch);
@@ -439,7 +447,7 @@ int unipool_rmsnorm_bwd(unipool_ctx* ctx, const void* dh, const void* r, int32_t
 
 int unipool_quantize_rows(unipool_ctx* ctx, const void* x, int32_t rows, int32_t width, uint8_t* q, float* q_scale,
                           unipool_stream stream) {
-  CHECK_CTX(ctx); CHECK_WIDTH(width);
+  CHECK_CTX(ctx); CHECK_DEVICE(ctx); CHECK_WIDTH(width);
   UP_REQUIRE(rows >= 0, UNIPOOL_ERR_INVALID_ARG, "rows = %d is negative", rows);
   CHECK_PTR(x); CHECK_PTR(q); CHECK_PTR(q_scale);
   return quantize_rows_launch(ctx, x, rows, width, q, q_scale, static_cast<cudaStream_t>(stream));
@@ -467,14 +475,14 @@ static int linear_call(unipool_ctx* ctx, const LinearArgs& a, unipool_stream str
 
 int unipool_linear(unipool_ctx* ctx, const void* x, int32_t T, int32_t n_in, const void* W, int32_t n_out,
                    const float* bias, int32_t act, const void* residual, void* pre, void* y, unipool_stream stream) {
-  CHECK_CTX(ctx);
+  CHECK_CTX(ctx); CHECK_DEVICE(ctx);
   return linear_call(ctx, LinearArgs{x, W, nullptr, nullptr, T, n_in, n_out, act, bias, residual, pre, y}, stream);
 }
 
 int unipool_linear_scaled(unipool_ctx* ctx, const uint8_t* x, const float* x_scale, int32_t T, int32_t n_in,
                           const uint8_t* W, const float* w_scale, int32_t n_out, const float* bias, int32_t act,
                           const void* residual, void* pre, void* y, unipool_stream stream) {
-  CHECK_CTX(ctx); CHECK_PTR(x_scale); CHECK_PTR(w_scale);
+  CHECK_CTX(ctx); CHECK_DEVICE(ctx); CHECK_PTR(x_scale); CHECK_PTR(w_scale);
   UP_REQUIRE(use_tensor_cores(ctx), UNIPOOL_ERR_UNSUPPORTED, "8-bit operands need a bf16 context");
   return linear_call(ctx, LinearArgs{x, W, x_scale, w_scale, T, n_in, n_out, act, bias, residual, pre, y}, stream);
 }
@@ -487,7 +495,7 @@ size_t unipool_linear_bwd_scratch(const unipool_ctx* ctx, int32_t T, int32_t n_i
 int unipool_linear_bwd(unipool_ctx* ctx, const void* dy, int32_t T, int32_t n_out, const void* pre, int32_t act,
                        const void* x, int32_t n_in, const void* W, void* dp, const void* dx_residual, void* dx, float* dW,
                        float* dbias, void* scratch, int32_t flags, unipool_stream stream) {
-  CHECK_CTX(ctx); CHECK_T(ctx, T); CHECK_FEATURES(n_in); CHECK_FEATURES(n_out); CHECK_ACT(act);
+  CHECK_CTX(ctx); CHECK_DEVICE(ctx); CHECK_T(ctx, T); CHECK_FEATURES(n_in); CHECK_FEATURES(n_out); CHECK_ACT(act);
   CHECK_PTR(dy);
   if (act != UNIPOOL_ACT_NONE) { CHECK_PTR(pre); CHECK_PTR(dp); }
   UP_REQUIRE(dx != nullptr || dW != nullptr || dbias != nullptr, UNIPOOL_ERR_INVALID_ARG, "dx, dW and dbias are all NULL");

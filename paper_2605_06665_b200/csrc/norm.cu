@@ -1,8 +1,9 @@
 // RMS norm of a residual stream, with the addition in front of it and 8-bit output behind it, and its backward pass.
 //
 //   r = x + y,  n_t = 1 / sqrt(mean_j r_tj^2 + eps),  h = r n_t w;   q = e4m3(h / s_t),  s_t = max_j |h_tj| / 448
-//   backward of h (gradient dh) and of r itself (dr):  with c_t = sum_j dh_tj w_j r_tj,
-//     dx = n_t w dh - r n_t^3 c_t / width + dr,        dw_j += sum_t dh_tj n_t r_tj
+//   backward of h (gradient dh) and of r itself (dr):  with xhat = r n_t,
+//     dx = n_t (w dh - xhat mean_j(w dh xhat)) + dr,   dw_j += sum_t dh_tj xhat_tj
+// (xhat is of size one whatever the row's scale: no power of n_t over- or underflows)
 //
 // Bound by HBM: forward 2 (x, h) to 4 (y, r too) passes over the stream, backward 3 to 4, next to no arithmetic.  A row stays
 // in the registers of the threads that share it, so that it is read once: a warp up to 256 vectors of 16 bytes (2048 bf16
@@ -206,10 +207,10 @@ template <int R> __device__ __forceinline__ int row_of_lane(int lane) { return l
 
 // A block takes R rows at a time and a thread VPT vectors of the same columns of each: it keeps w and its sums for dw in
 // registers over all its rows, and the rows' dot products cost one barrier for R of them.  (With a row to a warp the sums of a whole
-// row lay in every warp's registers, and they had to be added up at the end: 16384 rows of 768 bf16 22.5 us instead of 19.5, and more to add up behind it.)
+// row lay in every warp's registers and had to be added up at the end: 16384 rows of 768 bf16 22.5 us instead of 18.7.)
 // kRing: R rows are one run of bytes in memory; runs are copied, from the 16-byte boundary below to the one above, into a ring in
-// shared memory some stages ahead, so that reads go on while rows are worked on and whatever the rows' alignment (16384 rows of 770 bf16 read
-// element by element 69 us, through the ring 37).  Without it (arrays off 16 bytes, rows too long for two stages) the loads go
+// shared memory some stages ahead, so that reads go on while rows are worked on and whatever the rows' alignment (16384 rows of
+// 770 bf16 read element by element 69 us, through the ring 37).  Without it (arrays off 16 bytes, rows too long for two stages) the loads go
 // from memory into registers.
 // The sums' order depends on the sizes alone.
 template <typename E, int V, int VPT, int R, bool kRing>
@@ -335,8 +336,9 @@ __global__ void __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_
         if (!kKeepW) load_w<V>(p.w + c, wi);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          dw[i][j] = fmaf(u[j], v[j] * n[k], dw[i][j]);
-          dot[k] = fmaf(u[j] * wi[j], v[j], dot[k]);
+          const float xhat = v[j] * n[k];
+          dw[i][j] = fmaf(u[j], xhat, dw[i][j]);
+          dot[k] = fmaf(u[j] * wi[j], xhat, dot[k]);
         }
       }
     }
@@ -375,7 +377,7 @@ __global__ void __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       if (row0 + k >= p.T) break;
-      const float s = n[k] * n[k] * n[k] * (dot[k] * inv_width);
+      const float mean = dot[k] * inv_width;
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
         const int c = column(i);
@@ -386,7 +388,7 @@ __global__ void __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_
         float(&wi)[V] = w[kKeepW ? i : 0];
         if (!kKeepW) load_w<V>(p.w + c, wi);
 #pragma unroll
-        for (int j = 0; j < V; ++j) u[j] = n[k] * wi[j] * u[j] - v[j] * s;
+        for (int j = 0; j < V; ++j) u[j] = n[k] * (wi[j] * u[j] - v[j] * n[k] * mean);
         if (p.dr != nullptr) {
           d[k][i].get(v);
 #pragma unroll
@@ -457,8 +459,8 @@ template <bool kNorm, typename E> int norm_as(unipool_ctx* ctx, const NormParams
   auto run = [&](auto v, auto tpr, auto vpt) {
     constexpr int kTpr = decltype(tpr)::value, kRows = kNormThreads<kTpr> / kTpr;
     PhaseTimer pt(ctx, UNIPOOL_PH_RMSNORM, 1, s);
-    UP_KERNEL((rmsnorm_kernel<E, decltype(v)::value, kTpr, decltype(vpt)::value, kNorm>), (p.T + kRows - 1) / kRows, kNormThreads<kTpr>,
-              0, s, p);
+    UP_KERNEL((rmsnorm_kernel<E, decltype(v)::value, kTpr, decltype(vpt)::value, kNorm>), (unsigned)(((int64_t)p.T + kRows - 1) / kRows),
+              kNormThreads<kTpr>, 0, s, p);
     return UNIPOOL_OK;
   };
   // vectors of v elements whose number and rows' alignment allow them

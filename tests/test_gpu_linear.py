@@ -160,6 +160,37 @@ def test_forward_epilogues(mode, act, bias, residual, T):
     f.check(y, pre)
 
 
+@pytest.mark.parametrize("act,bias,residual,with_pre", [("none", False, False, False), ("gelu", True, False, True), ("silu", False, True, False),
+                                                         ("gelu", True, True, True), ("relu", True, True, False)])
+def test_forward_of_many_tokens(mode, act, bias, residual, with_pre):
+    """Several rounds of the widest tiles, a ragged last one; in place where there is a residual."""
+    T, n_in, n_out = 8003, 256, 2112
+    f = Forward(mode, T, n_in, n_out, act, bias, residual, seed=15)
+    yw, y = guarded((T, n_out), mode.dt)
+    pw, pre = guarded((T, n_out), mode.dt)
+    f.call(y, pre if with_pre else None)
+    f.check(y, pre if with_pre else None)
+    assert untouched(yw, y) and untouched(pw, pre)
+    if residual:
+        z = f.res.clone()
+        f.call(z, pre if with_pre else None, res=z)
+        assert torch.equal(z, y)
+
+
+def test_backward_of_many_tokens(train):
+    m, T, n_in, n_out = train, 8003, 2112, 256
+    d = backward_case(m, T, n_in, n_out, "relu", seed=25)
+    xw, dx = guarded((T, n_in), m.dt)
+    ww, dW = guarded((n_out, n_in), torch.float32)
+    db = torch.empty(n_out, device="cuda")
+    call_backward(m, d, T, n_in, n_out, "relu", dx, dW, db)
+    check_backward(m, d, T, "relu", dx, dW, db)
+    assert untouched(xw, dx) and untouched(ww, dW)
+    res = d["res"].clone()
+    call_backward(m, d, T, n_in, n_out, "relu", res, None, None, res=res)
+    assert torch.equal(res, dx)
+
+
 @pytest.mark.parametrize("T", [3, 700])
 def test_residual_in_place_and_fewer_tokens(mode, T):
     f = Forward(mode, T, 128, 320, "gelu", seed=7)
@@ -303,6 +334,21 @@ def test_gradients_by_differences(train):
         hi[which][at] += h
         want = (loss(*hi) - loss(*lo)) / (2 * h)
         assert abs(out[at].double() - want) <= tol
+
+
+def test_scratch_of_the_callers(train):
+    m = train
+    for T, n_in, n_out in ((40, 64, 64), (700, 128, 192), (3000, 64, 320)):
+        d = backward_case(m, T, n_in, n_out, "relu", seed=81)
+        n = m.ctx.linear_bwd_scratch(T, n_in, n_out)
+        out = [[torch.empty(n_out, n_in, device="cuda"), torch.empty(n_out, device="cuda")] for _ in range(2)]
+        whole = torch.full((n + 64,), 7, dtype=torch.uint8, device="cuda")
+        for o, scratch in zip(out, (None, whole[:n])):
+            m.ctx.linear_bwd(d["dy"], T, n_out, d["pre"], 1, d["x"], n_in, d["W"], d["dp"], None, None, *o, m.B.WGRAD_OVERWRITE, scratch)
+        assert all(torch.equal(a, b) for a, b in zip(*out)) and (whole[n:] == 7).all()
+        if n:
+            with pytest.raises(ValueError):
+                m.ctx.linear_bwd(d["dy"], T, n_out, d["pre"], 1, d["x"], n_in, d["W"], d["dp"], None, None, *out[0], 2, whole[:n - 1])
 
 
 def test_no_tokens(train):

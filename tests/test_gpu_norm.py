@@ -229,6 +229,41 @@ def test_special_rows(mode, width):
     assert torch.isnan(rstd[4]) and torch.isnan(h[4]).all() and torch.isnan(scale[4]) and torch.isnan(q[4].float()).all()
 
 
+@pytest.mark.parametrize("scale", [2.0 ** -60, 2.0 ** 40])
+def test_backward_of_tiny_and_large_rows(mode, scale):
+    """The cube of 1 / |r| passes fp32's range, the gradient does not."""
+    ctx, dt = mode
+    from paper_2605_06665_b200 import binding as B
+    T, width = 40, 768
+    r, dh = (normal((T, width), torch.float32, 50) * scale).to(dt), normal((T, width), dt, 51)
+    w = 1 + normal((width,), torch.float32, 52, 0.2)
+    rstd = ((r.double() ** 2).mean(1) ** -0.5).float()
+    dx, dw = torch.empty_like(r), torch.empty_like(w)
+    ctx.rmsnorm_bwd(dh, r, T, width, w, rstd, None, dx, dw, B.WGRAD_OVERWRITE)
+    n, xhat, g = rstd.double()[:, None], r.double() * rstd.double()[:, None], dh.double() * w.double()
+    want = n * (g - xhat * (g * xhat).mean(1, keepdim=True))
+    size = n * (g.abs() + xhat.abs() * (g * xhat).abs().mean(1, keepdim=True))
+    assert torch.isfinite(dx).all()
+    assert ((dx.double() - want).abs() <= half_step(dt) * want.abs() + FP32 * size).all()
+    terms = dh.double() * xhat
+    assert ((dw.double() - terms.sum(0)).abs() <= (T + 8) * 2.0 ** -24 * terms.abs().sum(0)).all()
+
+
+def test_scratch_of_the_callers(mode):
+    ctx, dt = mode
+    T, width = 500, 768
+    dh, r, w, rstd = normal((T, width), dt, 53), normal((T, width), dt, 54), torch.ones(width, device="cuda"), torch.ones(T, device="cuda")
+    n = ctx.rmsnorm_bwd_scratch(T, width)
+    want, got = (torch.zeros(width, device="cuda") for _ in range(2))
+    dx = torch.empty_like(dh)
+    ctx.rmsnorm_bwd(dh, r, T, width, w, rstd, None, dx, want)
+    whole = torch.full((n + 64,), 7, dtype=torch.uint8, device="cuda")
+    ctx.rmsnorm_bwd(dh, r, T, width, w, rstd, None, dx, got, scratch=whole[:n])
+    assert torch.equal(got, want) and (whole[n:] == 7).all()
+    with pytest.raises(ValueError):
+        ctx.rmsnorm_bwd(dh, r, T, width, w, rstd, None, dx, got, scratch=whole[:n - 1])
+
+
 def test_no_rows(mode):
     ctx, dt = mode
     from paper_2605_06665_b200 import binding as B

@@ -23,8 +23,10 @@ def lib(tmp_path_factory):
     names = [line.split()[-1] for line in subprocess.run(["nm", "-u", obj], check=True, capture_output=True, text=True).stdout.splitlines()]
     stubs = [n for n in names if n.startswith(("_ZN7unipool", "cuda", "__cuda"))]
     assert any("rmsnorm_launch" in n for n in stubs) and any("linear_bwd_launch" in n for n in stubs)
-    # (the launchers return 0, the sizes of scratch 64)
-    (d / "stubs.s").write_text(".text\n" + "".join(f".globl {n}\n{n}:\n  movl ${64 if '_scratch' in n else 0}, %eax\n  ret\n" for n in stubs)
+    # (the launchers return 0, the sizes of scratch 64; the current device is the variable fake_device)
+    stubs.remove("cudaGetDevice")
+    (d / "stubs.s").write_text(".globl fake_device\n.data\nfake_device: .long 0\n.text\n.globl cudaGetDevice\ncudaGetDevice:\n"
+                               "  movl fake_device(%rip), %eax\n  movl %eax, (%rdi)\n  xorl %eax, %eax\n  ret\n" + "".join(f".globl {n}\n{n}:\n  movl ${64 if '_scratch' in n else 0}, %eax\n  ret\n" for n in stubs)
                                + '.section .note.GNU-stack,"",@progbits\n')
     so = str(d / "checks.so")
     subprocess.run(["g++", "-shared", "-Wl,-Bsymbolic", obj, str(d / "stubs.s"), "-o", so], check=True)
@@ -153,3 +155,26 @@ def test_linear_backward(lib, ctx):
 def test_scratch_sizes_of_nothing(lib, ctx):
     assert lib.unipool_rmsnorm_bwd_scratch(None, 10, 768) == 0 and lib.unipool_rmsnorm_bwd_scratch(ctx, 0, 768) == 0
     assert lib.unipool_linear_bwd_scratch(None, 10, 64, 64) == 0 and lib.unipool_linear_bwd_scratch(ctx, 10, 65, 64) == 0
+
+
+def test_another_device_is_current(lib, ctx):
+    device = ctypes.c_int.in_dll(lib, "fake_device")
+    calls = [("rmsnorm", norm_args(ctx)), ("linear", linear_args(ctx))]
+    try:
+        device.value = 1
+        for name, args in calls:
+            assert call(lib, name, args) == ARG and b"device" in lib.unipool_last_error()
+        assert lib.unipool_quantize_rows(ctx, P, 10, 64, P, P, None) == ARG
+    finally:
+        device.value = 0
+    for name, args in calls:
+        assert call(lib, name, args) == 0
+
+
+def test_binding_takes_dense_tensors_only():
+    torch = pytest.importorskip("torch")
+    a = torch.zeros(4, 6)
+    assert B._d(a) == a.data_ptr() and B._d(a[1:3]) == a[1:3].data_ptr() and B._d(None) is None
+    for t in (a.t(), a[:, :3], a[::2], a[0].expand(4, 6)):
+        with pytest.raises(ValueError):
+            B._d(t)
