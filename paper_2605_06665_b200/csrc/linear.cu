@@ -164,26 +164,30 @@ struct SimtLinear {
   bool vec_a, vec_b, vec_c, add;                         // 16-byte aligned operands; vec_c: everything of the epilogue
 };
 
+template <typename Tile> constexpr int tile_cols = kSimtN;
+template <> constexpr int tile_cols<SimtWideTile> = SimtWideTile::kCols;
+
 // C = act(A B + bias) + residual; B along K (forward) or across it (dx).  S blocks of a cluster share a tile by taking runs of its
 // contraction and add up through each other's shared memory, in the order of their ranks (few tiles of a long contraction leave
-// most SMs idle otherwise: 16 tokens 2048 -> 1728 35 us with one block to a tile, XX with eight).
+// most SMs idle otherwise: 16 tokens 2048 -> 1728 35 us with one block to a tile, 12 with eight).
 template <typename Tile, Major BM, int S>
 __global__ void __cluster_dims__(1, 1, S) __launch_bounds__(Tile::kThreads, Tile::kBlocks) linear_rows_kernel(SimtLinear p) {
   grid_wait(p.A, p.B, p.bias, p.residual);
   extern __shared__ float4 smem_raw[];
   typename Tile::Smem& sm = *reinterpret_cast<typename Tile::Smem*>(smem_raw);
-  const int m0 = blockIdx.x * Tile::kRows, n0 = blockIdx.y * kSimtN;
+  const int m0 = blockIdx.x * Tile::kRows, n0 = blockIdx.y * tile_cols<Tile>;
   const int all = p.K / kSimtKC, c0 = all * (int)blockIdx.z / S, c1 = all * ((int)blockIdx.z + 1) / S;
   Tile t;
   t.template run<kAlongK, BM>(
       sm, c1 - c0, p.vec_a, p.vec_b, p.A, [](int) {},
       [&](int c, int i, int k) { return m0 + i < p.M ? p.A + (int64_t)(m0 + i) * p.K + (c0 + c) * kSimtKC + k : nullptr; },
-      [&](int c, int i, int k) {
+      [&](int c, int i, int k) -> const float* {
         const int kk = (c0 + c) * kSimtKC + k;
+        if (tile_cols<Tile> > kSimtN && n0 + i >= p.N) return nullptr;
         return BM == kAlongK ? p.B + (int64_t)(n0 + i) * p.K + kk : p.B + (int64_t)kk * p.N + n0 + i;
       });
   auto put = [&](int i, int j, float4 v) {
-    if (m0 + i >= p.M) return;
+    if (m0 + i >= p.M || (tile_cols<Tile> > kSimtN && n0 + j >= p.N)) return;
     const int n = n0 + j;
     const int64_t at = (int64_t)(m0 + i) * p.N + n;
     if (p.bias != nullptr) {
@@ -256,7 +260,7 @@ template <typename Tile, Major BM, int S> int rows_as(unipool_ctx* ctx, int phas
   auto kern = linear_rows_kernel<Tile, BM, S>;
   constexpr int smem = (int)sizeof(typename Tile::Smem);
   UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, smem));
-  UP_KERNEL(kern, dim3((p.M + Tile::kRows - 1) / Tile::kRows, p.N / kSimtN, S), Tile::kThreads, smem, s, p);
+  UP_KERNEL(kern, dim3((p.M + Tile::kRows - 1) / Tile::kRows, (p.N + tile_cols<Tile> - 1) / tile_cols<Tile>, S), Tile::kThreads, smem, s, p);
   return UNIPOOL_OK;
 }
 template <Major BM> int rows_simt(unipool_ctx* ctx, int phase, const SimtLinear& p, cudaStream_t s) {
@@ -271,24 +275,31 @@ template <Major BM> int rows_simt(unipool_ctx* ctx, int phase, const SimtLinear&
     if (fits(2)) return rows_as<SimtTile<4>, BM, 2>(ctx, phase, p, s);
   }
   if (tiles <= ctx->sm_count) return rows_as<SimtTile<8>, BM, 1>(ctx, phase, p, s);
+  // us, forward and dx, tiles of 128 x 128 / the others: 4000 tokens 1024 -> 1024 213/244, 201/224; 16384 768 -> 1024 536/585, 566/571;
+  // 3000 4096 -> 1536 798/878, 842/842; 8000 1024 -> 1024 415/400, 391/377 (1.7 rounds of blocks)
+  if ((int64_t)((p.M + 127) / 128) * ((p.N + 127) / 128) >= ctx->sm_count) return rows_as<SimtWideTile, BM, 1>(ctx, phase, p, s);
   if (tiles <= 6 * ctx->sm_count) return rows_as<SimtTile<4>, BM, 1>(ctx, phase, p, s);
   return rows_as<SimtBlockTile<1>, BM, 1>(ctx, phase, p, s);
 }
 
-// Parts of the tokens for the weight gradient: two blocks of tiles to an SM, 256 tokens at least to a part.
-int dw_splits_simt(const unipool_ctx* ctx, int T, int n_in, int n_out) {
+// Parts of the tokens for the weight gradient: two blocks of tiles to an SM, 256 tokens at least to a part.  (Tiles of 128 x 128 were no
+// faster: 16384 tokens 768 x 1024 622/622 us, 3000 of 4096 x 1536 807/770.)
+int dw_length_simt(const unipool_ctx* ctx, int T, int n_in, int n_out) {
   const int tiles = (n_out / 64) * (n_in / 64);
   int n = (2 * ctx->sm_count + tiles - 1) / tiles;
   if (n > (T + 255) / 256) n = (T + 255) / 256;
   if (n < 1) n = 1;
-  const int len = ((T + n - 1) / n + kSimtKC - 1) / kSimtKC * kSimtKC;
+  return ((T + n - 1) / n + kSimtKC - 1) / kSimtKC * kSimtKC;
+}
+int dw_splits_simt(const unipool_ctx* ctx, int T, int n_in, int n_out) {
+  const int len = dw_length_simt(ctx, T, n_in, n_out);
   return (T + len - 1) / len;
 }
 int dw_simt(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, float* out, int splits, bool add, cudaStream_t s) {
   SimtLinear p{};
   p.A = static_cast<const float*>(dp); p.B = static_cast<const float*>(a.x); p.C = out;
   p.M = a.n_out; p.N = a.n_in; p.K = a.T; p.add = add;
-  p.k_len = ((a.T + splits - 1) / splits + kSimtKC - 1) / kSimtKC * kSimtKC;
+  p.k_len = dw_length_simt(ctx, a.T, a.n_in, a.n_out);
   p.vec_a = aligned16(p.A); p.vec_b = aligned16(p.B); p.vec_c = aligned16(p.C);
   PhaseTimer pt(ctx, UNIPOOL_PH_LINEAR_BWD, 1, s);
   UP_CUDA(cudaFuncSetAttribute(linear_dw_kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)sizeof(LinearDwTile::Smem)));

@@ -337,4 +337,98 @@ struct SimtBlockTile {
   }
 };
 
+// The tile of large dense products: 128 x 128, 256 threads, 8 x 8 results a thread in packed pairs, a warp 32 rows of 64 columns (each
+// 16-byte load of a warp one pass through shared memory).  Half the bytes of the 64 x 64 tile per product come from L2.  FMA pipe busy
+// 69 to 72 % of the time, two blocks of eight warps to an SM (9472 tokens 1024 -> 1024, 50 TFLOP/s).
+struct SimtWideTile {
+  static constexpr int kThreads = 256, kBlocks = 2, kRows = 128, kCols = 128, MR = 8, NR = 8, kLd = 132;
+  static constexpr int k4 = kRows * kSimtKC / 4 / kThreads;        // float4 of an operand's chunk per thread
+  struct Smem { float a[2][kSimtKC][kLd], b[2][kSimtKC][kLd]; };
+  unsigned long long acc[MR][NR / 2];
+
+  __device__ static int row(int i) { return i % 4 + i / 4 * 64 + (threadIdx.x / 64 * 4 + threadIdx.x % 32 / 8) * 4; }
+  __device__ static int col(int j) { return j % 4 + j / 4 * 64 + (threadIdx.x / 32 % 2 * 8 + threadIdx.x % 8) * 4; }
+
+  template <Major MJ, typename F> __device__ static void fetch(float4 (&r)[k4], bool vec, F src) {
+#pragma unroll
+    for (int q = 0; q < k4; ++q) {
+      const int v = threadIdx.x + q * kThreads;
+      const float* p = MJ == kAlongK ? src(v / 4, v % 4 * 4) : src(v % 32 * 4, v / 32);
+      r[q] = p ? ld4(p, vec) : make_float4(0.f, 0.f, 0.f, 0.f);
+    }
+  }
+  template <Major MJ> __device__ static void stash(float (*s)[kLd], const float4 (&r)[k4]) {
+#pragma unroll
+    for (int q = 0; q < k4; ++q) {
+      const int v = threadIdx.x + q * kThreads;
+      if (MJ == kAlongK) {
+        const int i = v / 4, k = v % 4 * 4;
+        s[k][i] = r[q].x; s[k + 1][i] = r[q].y; s[k + 2][i] = r[q].z; s[k + 3][i] = r[q].w;
+      } else {
+        *reinterpret_cast<float4*>(&s[v / 32][v % 32 * 4]) = r[q];
+      }
+    }
+  }
+  struct Frag { float a[MR]; unsigned long long b[NR / 2]; };
+  __device__ static void read(Frag& f, const float (*sa)[kLd], const float (*sb)[kLd], int k) {
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const float4 v = *reinterpret_cast<const float4*>(&sa[k][row(4 * h)]);
+      f.a[4 * h] = v.x; f.a[4 * h + 1] = v.y; f.a[4 * h + 2] = v.z; f.a[4 * h + 3] = v.w;
+      const ulonglong2 w = *reinterpret_cast<const ulonglong2*>(&sb[k][col(4 * h)]);
+      f.b[2 * h] = w.x; f.b[2 * h + 1] = w.y;
+    }
+  }
+
+  // As SimtTile::run.
+  template <Major AM, Major BM, typename FB0, typename FA, typename FB>
+  __device__ void run(Smem& s, int n_chunks, bool vec_a, bool vec_b, const float*, FB0, FA a_at, FB b_at) {
+#pragma unroll
+    for (int i = 0; i < MR; ++i)
+#pragma unroll
+      for (int j = 0; j < NR / 2; ++j) acc[i][j] = 0ull;
+    float4 ra[k4], rb[k4];
+    auto load = [&](int c) {
+      fetch<AM>(ra, vec_a, [&](int i, int k) -> const float* { return a_at(c, i, k); });
+      fetch<BM>(rb, vec_b, [&](int i, int k) -> const float* { return b_at(c, i, k); });
+    };
+    if (n_chunks > 0) load(0);
+    for (int c = 0; c < n_chunks; ++c) {
+      float (*sa)[kLd] = s.a[c & 1];
+      float (*sb)[kLd] = s.b[c & 1];
+      stash<AM>(sa, ra);
+      stash<BM>(sb, rb);
+      __syncthreads();                             // also: everyone is done with the buffer the next chunk goes to
+      if (c + 1 < n_chunks) load(c + 1);
+      Frag f[2];
+      read(f[0], sa, sb, 0);
+#pragma unroll
+      for (int k = 0; k < kSimtKC; ++k) {
+        if (k + 1 < kSimtKC) read(f[(k + 1) & 1], sa, sb, k + 1);
+        const Frag& g = f[k & 1];
+#pragma unroll
+        for (int i = 0; i < MR; ++i) {
+          unsigned long long aa;
+          asm("mov.b64 %0, {%1, %1};" : "=l"(aa) : "f"(g.a[i]));
+#pragma unroll
+          for (int j = 0; j < NR / 2; ++j) asm("fma.rn.f32x2 %0, %1, %2, %0;" : "+l"(acc[i][j]) : "l"(aa), "l"(g.b[j]));
+        }
+      }
+    }
+  }
+  __device__ float4 value4(int i, int j) const {
+    auto one = [&](int jj) {
+      const unsigned long long v = acc[i][jj / 2];
+      return __uint_as_float(jj & 1 ? (uint32_t)(v >> 32) : (uint32_t)v);
+    };
+    return make_float4(one(j), one(j + 1), one(j + 2), one(j + 3));
+  }
+  template <typename F> __device__ void each4(const Smem&, F put) const {
+#pragma unroll
+    for (int i = 0; i < MR; ++i)
+#pragma unroll
+      for (int j = 0; j < NR; j += 4) put(row(i), col(j), value4(i, j));
+  }
+};
+
 }  // namespace unipool
