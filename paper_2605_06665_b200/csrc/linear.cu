@@ -275,9 +275,12 @@ template <Major BM> int rows_simt(unipool_ctx* ctx, int phase, const SimtLinear&
     if (fits(2)) return rows_as<SimtTile<4>, BM, 2>(ctx, phase, p, s);
   }
   if (tiles <= ctx->sm_count) return rows_as<SimtTile<8>, BM, 1>(ctx, phase, p, s);
-  // us, forward and dx, tiles of 128 x 128 / the others: 4000 tokens 1024 -> 1024 213/244, 201/224; 16384 768 -> 1024 536/585, 566/571;
-  // 3000 4096 -> 1536 798/878, 842/842; 8000 1024 -> 1024 415/400, 391/377 (1.7 rounds of blocks)
-  if ((int64_t)((p.M + 127) / 128) * ((p.N + 127) / 128) >= ctx->sm_count) return rows_as<SimtWideTile, BM, 1>(ctx, phase, p, s);
+  // Tiles of 128 x 128 where they give three of four SMs two blocks and little of them lies outside.  us, forward and dx, with / without:
+  // 4000 tokens 1024 -> 1024 213/244, 201/224; 16384 768 -> 1024 536/585, 566/571; 3000 4096 -> 1536 798/878, 842/842; 8000 1024 -> 1024
+  // 415/400, 391/377 (1.7 rounds of blocks)
+  const int64_t wide = (int64_t)((p.M + 127) / 128) * ((p.N + 127) / 128);
+  if (2 * wide >= 3 * ctx->sm_count && 20 * (int64_t)p.M * p.N >= 17 * wide * 128 * 128)
+    return rows_as<SimtWideTile, BM, 1>(ctx, phase, p, s);
   if (tiles <= 6 * ctx->sm_count) return rows_as<SimtTile<4>, BM, 1>(ctx, phase, p, s);
   return rows_as<SimtBlockTile<1>, BM, 1>(ctx, phase, p, s);
 }

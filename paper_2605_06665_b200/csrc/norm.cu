@@ -259,8 +259,14 @@ __global__ void __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_
     for (int j = 0; j < V; ++j) dw[i][j] = 0.f;
   if constexpr (kKeepW) {
 #pragma unroll
-    for (int i = 0; i < VPT; ++i)
+    for (int i = 0; i < VPT; ++i) {
+#pragma unroll
+      for (int j = 0; j < V; ++j) w[i][j] = 0.f;
       if (column(i) < p.width) load_w<V>(p.w + column(i), w[i]);
+    }
+  } else {
+#pragma unroll
+    for (int j = 0; j < V; ++j) w[0][j] = 0.f;
   }
   const float inv_width = 1.f / (float)p.width;
   int turn = 0, stage = 0;
@@ -271,11 +277,11 @@ __global__ void __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_
     for (int k = 0; k < R; ++k) n_next[k] = g * R + k < p.T ? __ldg(p.rstd + (g * R + k)) : 0.f;
   };
   load_rstd(blockIdx.x);
-  for (int64_t g = blockIdx.x; g < groups; g += gridDim.x, turn ^= 1) {
-    const int64_t row0 = g * R;
-    uint8_t* at_stage = ring + (size_t)stage * arrays * slot + g * run % 16;
+  for (int64_t group = blockIdx.x; group < groups; group += gridDim.x, turn ^= 1) {
+    const int64_t row0 = group * R;
+    uint8_t* at_stage = ring + (size_t)stage * arrays * slot + group * run % 16;
     if constexpr (kRing) {
-      if (end_of(g) <= total) {
+      if (end_of(group) <= total) {
         // (a wait that runs out is reported, and no later one waits; the block goes on to its end)
         if (!*abort && !tc::mbar_wait(&full[stage], phase, abort)) {
           *abort = 1;
@@ -292,16 +298,21 @@ __global__ void __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_
         __syncthreads();
       }
     }
-    Vec<E, V> a[R][VPT], b[R][VPT], d[R][VPT];
-    float n[R], dot[R];
+    // g = w dh and xhat stay in registers from one side of the barrier to the other
+    Vec<E, V> d[R][VPT];
+    float g[R][VPT][V], xhat[R][VPT][V], n[R], dot[R];
 #pragma unroll
     for (int k = 0; k < R; ++k) {
       const bool live = row0 + k < p.T;
+      n[k] = n_next[k];
+      dot[k] = 0.f;
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
         const int c = column(i);
-        a[k][i].zero();
-        b[k][i].zero();
+        Vec<E, V> a, b;
+        a.zero();
+        b.zero();
+        d[k][i].zero();
         if (live && c < p.width) {
           const E *x, *y, *z;
           if constexpr (kRing) {
@@ -314,41 +325,36 @@ __global__ void __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_
             y = static_cast<const E*>(p.r) + at;
             z = static_cast<const E*>(p.dr) + at;
           }
-          a[k][i].load(x);
-          b[k][i].load(y);
+          a.load(x);
+          b.load(y);
           if (p.dr != nullptr) d[k][i].load(z);
         }
+        a.get(g[k][i]);
+        b.get(xhat[k][i]);
       }
-      n[k] = n_next[k];
     }
-    load_rstd(g + gridDim.x);
+    load_rstd(group + gridDim.x);
 #pragma unroll
-    for (int k = 0; k < R; ++k) {
-      dot[k] = 0.f;
+    for (int k = 0; k < R; ++k)
 #pragma unroll
       for (int i = 0; i < VPT; ++i) {
-        const int c = column(i);
-        if (c >= p.width) continue;
-        float u[V], v[V];
-        a[k][i].get(u);
-        b[k][i].get(v);
         float(&wi)[V] = w[kKeepW ? i : 0];
-        if (!kKeepW) load_w<V>(p.w + c, wi);
+        if (!kKeepW && column(i) < p.width) load_w<V>(p.w + column(i), wi);
 #pragma unroll
         for (int j = 0; j < V; ++j) {
-          const float xhat = v[j] * n[k];
-          dw[i][j] = fmaf(u[j], xhat, dw[i][j]);
-          dot[k] = fmaf(u[j] * wi[j], xhat, dot[k]);
+          xhat[k][i][j] *= n[k];
+          dw[i][j] = fmaf(g[k][i][j], xhat[k][i][j], dw[i][j]);
+          g[k][i][j] *= wi[j];
+          dot[k] = fmaf(g[k][i][j], xhat[k][i][j], dot[k]);
         }
       }
-    }
     {
       const float sum = reduce_rows<R>(dot, t % 32);
       if (t % (32 / R) == 0) part[turn][t / 32][row_of_lane<R>(t % 32)] = sum;
     }
     __syncthreads();                                     // (two arrays in turn: the next rows' sums need no second barrier)
     if constexpr (kRing) {                               // the stage is in registers: on to the rows that lie `stages` further
-      if (t == 0 && g + (int64_t)p.stages * gridDim.x < groups && !*abort) fetch(g + (int64_t)p.stages * gridDim.x, stage);
+      if (t == 0 && group + (int64_t)p.stages * gridDim.x < groups && !*abort) fetch(group + (int64_t)p.stages * gridDim.x, stage);
       if (++stage == p.stages) { stage = 0; phase ^= 1u; }
     }
     if (n_warps <= 4) {
@@ -382,18 +388,10 @@ __global__ void __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_
       for (int i = 0; i < VPT; ++i) {
         const int c = column(i);
         if (c >= p.width) continue;
-        float u[V], v[V];
-        a[k][i].get(u);
-        b[k][i].get(v);
-        float(&wi)[V] = w[kKeepW ? i : 0];
-        if (!kKeepW) load_w<V>(p.w + c, wi);
+        float u[V];
+        d[k][i].get(u);                                  // (zeros without dr)
 #pragma unroll
-        for (int j = 0; j < V; ++j) u[j] = n[k] * (wi[j] * u[j] - v[j] * n[k] * mean);
-        if (p.dr != nullptr) {
-          d[k][i].get(v);
-#pragma unroll
-          for (int j = 0; j < V; ++j) u[j] += v[j];
-        }
+        for (int j = 0; j < V; ++j) u[j] = fmaf(n[k], fmaf(-xhat[k][i][j], mean, g[k][i][j]), u[j]);
         Vec<E, V>::store(static_cast<E*>(p.dx) + (row0 + k) * p.width + c, u);
       }
     }
