@@ -4,6 +4,7 @@
 //   backward  dp = dy act'(p),  dx = dp W (+ dx_residual),  dW (+)= dp^T x,  dbias (+)= sum_t dp
 #include <cooperative_groups.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "common.cuh"
@@ -18,7 +19,8 @@ namespace {
 // ---------------------------------------------------------------- dp and the sums for dbias
 // dp = dy act'(p), rounded to the element type, and the column sums of the unrounded dp over the block's rows, into parts
 // [gridDim.y, N] (one row block: the gradient itself).  A thread owns V columns and every eighth row of the block's run;
-// eight rows' threads are added up in their order.  Bound by HBM (dy, p in, dp out).
+// eight rows' threads are added up in their order.  Bound by HBM (dy, p in, dp out: 201 MB of 16384 x 2048 bf16 in 29 us, 7 TB/s with
+// part of dp still in L2), with silu and gelu by the special-function unit beside it (two instructions an element, 15 us).
 constexpr int kDpRows = 8, kDpAhead = 4;                 // rows of a block's warps, rows that each has in flight
 
 struct DpParams {
@@ -28,6 +30,38 @@ struct DpParams {
   int T, N, rows, act;                                   // rows: of a block's run
   bool add;                                              // one row block: dbias +=
 };
+
+// the rows of a thread, from t on
+template <typename E, int V, bool kFast, int ACT>
+__device__ __forceinline__ void dp_run(const DpParams& a, int t, int t1, int c, float (&sum)[V]) {
+  const E* gy = static_cast<const E*>(a.dy) + c;
+  const E* gp = static_cast<const E*>(a.p) + c;
+  for (; t < t1; t += kDpRows * kDpAhead) {
+    Vec<E, V> dy[kDpAhead], pre[kDpAhead];
+#pragma unroll
+    for (int u = 0; u < kDpAhead; ++u) {
+      const int row = t + u * kDpRows;
+      dy[u].zero();
+      if (row >= t1) continue;
+      dy[u].load(gy + (int64_t)row * a.N);
+      if (ACT != UNIPOOL_ACT_NONE) pre[u].load(gp + (int64_t)row * a.N);
+    }
+#pragma unroll
+    for (int u = 0; u < kDpAhead; ++u) {
+      const int row = t + u * kDpRows;
+      float d[V], p[V];
+      dy[u].get(d);
+      if (ACT != UNIPOOL_ACT_NONE && row < t1) {
+        pre[u].get(p);
+#pragma unroll
+        for (int j = 0; j < V; ++j) d[j] *= act_slope<kFast>(p[j], ACT);
+        Vec<E, V>::store(static_cast<E*>(a.dp) + ((int64_t)row * a.N + c), d);
+      }
+#pragma unroll
+      for (int j = 0; j < V; ++j) sum[j] += d[j];
+    }
+  }
+}
 
 template <typename E, int V, bool kFast>
 __global__ void __launch_bounds__(256) linear_dp_kernel(DpParams a) {
@@ -39,29 +73,11 @@ __global__ void __launch_bounds__(256) linear_dp_kernel(DpParams a) {
 #pragma unroll
   for (int j = 0; j < V; ++j) sum[j] = 0.f;
   if (c < a.N) {
-    for (int t = t0 + g; t < t1; t += kDpRows * kDpAhead) {
-      Vec<E, V> dy[kDpAhead], pre[kDpAhead];
-#pragma unroll
-      for (int u = 0; u < kDpAhead; ++u) {
-        const int64_t at = (int64_t)(t + u * kDpRows) * a.N + c;
-        dy[u].zero();
-        if (t + u * kDpRows >= t1) continue;
-        dy[u].load(static_cast<const E*>(a.dy) + at);
-        if (a.dp != nullptr) pre[u].load(static_cast<const E*>(a.p) + at);
-      }
-#pragma unroll
-      for (int u = 0; u < kDpAhead; ++u) {
-        float d[V], p[V];
-        dy[u].get(d);
-        if (a.dp != nullptr && t + u * kDpRows < t1) {
-          pre[u].get(p);
-#pragma unroll
-          for (int j = 0; j < V; ++j) d[j] *= act_slope<kFast>(p[j], a.act);
-          Vec<E, V>::store(static_cast<E*>(a.dp) + (int64_t)(t + u * kDpRows) * a.N + c, d);
-        }
-#pragma unroll
-        for (int j = 0; j < V; ++j) sum[j] += d[j];
-      }
+    switch (a.act) {
+      case UNIPOOL_ACT_NONE: dp_run<E, V, kFast, UNIPOOL_ACT_NONE>(a, t0 + g, t1, c, sum); break;
+      case UNIPOOL_ACT_RELU: dp_run<E, V, kFast, UNIPOOL_ACT_RELU>(a, t0 + g, t1, c, sum); break;
+      case UNIPOOL_ACT_SILU: dp_run<E, V, kFast, UNIPOOL_ACT_SILU>(a, t0 + g, t1, c, sum); break;
+      case UNIPOOL_ACT_GELU: dp_run<E, V, kFast, UNIPOOL_ACT_GELU>(a, t0 + g, t1, c, sum); break;
     }
   }
   if (a.parts == nullptr) return;
@@ -81,12 +97,13 @@ __global__ void __launch_bounds__(256) linear_dp_kernel(DpParams a) {
 
 // Rows of each of n row blocks: whole steps of the loop.
 int dp_rows(int T, int n) { return ((T + n - 1) / n + kDpRows * kDpAhead - 1) / (kDpRows * kDpAhead) * (kDpRows * kDpAhead); }
-// Row blocks of the kernel: so many that four blocks lie on an SM, of 32 rows at least; few rows on one, which leaves nothing to
-// add up behind it.
-int dp_row_blocks(const unipool_ctx* ctx, int T, int N, int cols_per_block) {
+// Row blocks of the kernel, of 32 rows at least: four blocks to an SM, as its registers allow, where the special-function unit is to be
+// kept busy, three where the rows' bytes are all (16384 x 2048 bf16 with the sum behind it: gelu 35.4 us with four and 37.4 with
+// three, relu 35.0 and 33.3); few rows on one, which leaves nothing to add up behind it.
+int dp_row_blocks(const unipool_ctx* ctx, int T, int N, int cols_per_block, int act) {
   const int across = (N + cols_per_block - 1) / cols_per_block;
   if (T <= 3 * kDpRows * kDpAhead) return 1;
-  int n = 4 * ctx->sm_count / across;
+  int n = (act == UNIPOOL_ACT_SILU || act == UNIPOOL_ACT_GELU ? 4 : 3) * ctx->sm_count / across;
   if (n > (T + 31) / 32) n = (T + 31) / 32;
   if (n < 1) n = 1;
   return (T + dp_rows(T, n) - 1) / dp_rows(T, n);
@@ -320,7 +337,7 @@ int dw_splits(const unipool_ctx* ctx, int T, int n_in, int n_out) {
 
 template <typename E, int V, bool kFast>
 int dp_as(unipool_ctx* ctx, const LinearBwdArgs& a, int* blocks, float* parts, cudaStream_t s) {
-  const int n = dp_row_blocks(ctx, a.T, a.n_out, 32 * V);
+  const int n = dp_row_blocks(ctx, a.T, a.n_out, 32 * V, a.act);
   DpParams p{a.dy, a.pre, a.act != UNIPOOL_ACT_NONE ? a.dp : nullptr, nullptr, a.T, a.n_out, dp_rows(a.T, n), a.act, false};
   if (a.dbias != nullptr) {
     p.parts = n > 1 ? parts : a.dbias;
@@ -355,9 +372,10 @@ static size_t dw_parts(const unipool_ctx* ctx, int T, int n_in, int n_out) {
   return splits > 1 ? (size_t)splits * n_in * n_out : 0;
 }
 size_t linear_bwd_scratch(const unipool_ctx* ctx, int T, int n_in, int n_out) {
-  const int n = dp_row_blocks(ctx, T, n_out, 32 * (tensor_cores(ctx) ? 8 : 4)), m = dp_row_blocks(ctx, T, n_out, 32);
-  const size_t sums = n > m ? n : m;
-  return (dw_parts(ctx, T, n_in, n_out) + (sums > 1 ? sums * n_out : 0)) * sizeof(float);
+  int sums = 0;                                          // (the widest call: any activation, and in fp32 any alignment)
+  for (const int act : {UNIPOOL_ACT_NONE, UNIPOOL_ACT_GELU})
+    for (const int cols : {32 * (tensor_cores(ctx) ? 8 : 4), 32}) sums = std::max(sums, dp_row_blocks(ctx, T, n_out, cols, act));
+  return (dw_parts(ctx, T, n_in, n_out) + (sums > 1 ? (size_t)sums * n_out : 0)) * sizeof(float);
 }
 
 int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) {

@@ -42,9 +42,11 @@ template <bool kFast> __device__ __forceinline__ float act_slope(float p, int ac
       return s * (1.f + p * (1.f - s));
     }
     case UNIPOOL_ACT_GELU: {
-      const float q = p > 30.f ? 30.f : p < -30.f ? -30.f : p;      // 0 or 1 from there on; the square would overflow
-      const float s = logistic<kFast>(kGeluTwice * (q + kGeluCube * q * q * q));
-      return s + q * s * (1.f - s) * kGeluTwice * (1.f + 3.f * kGeluCube * q * q);
+      const float q = fminf(fmaxf(p, -30.f), 30.f), q2 = q * q;     // 0 or 1 from there on; the square would overflow
+      float s;                                                      // (p itself carries a NaN into s)
+      if constexpr (kFast) s = rcp_1_ex2(p * fmaf(q2, -kLog2e * kGeluTwice * kGeluCube, -kLog2e * kGeluTwice));
+      else s = logistic<false>(kGeluTwice * (p + kGeluCube * p * q2));
+      return fmaf(fmaf(-s, s, s), q * fmaf(q2, 3.f * kGeluTwice * kGeluCube, kGeluTwice), s);
     }
     default: return 1.f;
   }
