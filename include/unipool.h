@@ -419,7 +419,8 @@ int unipool_linear_scaled(unipool_ctx* ctx, const uint8_t* x, const float* x_sca
 /* Backward of unipool_linear:
  *   dp = dy act'(p);  dx = dp W (+ dx_residual);  dW += dp^T x;  dbias += sum_t dp
  * (the residual's gradient is dy).  dp is rounded to the ctx dtype, as an operand of both products; dbias sums the
- * unrounded values.  Sums are taken in an order that depends on the sizes alone.
+ * unrounded values.  Sums are taken in an order that depends on the sizes, the activation and which of dx and dW are asked
+ * for alone (together they may share a launch, cut into other parts).
  * in : dy [T,n_out]; pre [T,n_out] of the forward call and dp [T,n_out], scratch that is overwritten (both NULL
  *      with UNIPOOL_ACT_NONE; dp may be pre or dy); x, W of the forward call (x is needed for dW, W for dx);
  *      dx_residual [T,n_in] or NULL; scratch: unipool_linear_bwd_scratch() bytes of device memory, 16-byte aligned,

@@ -263,8 +263,9 @@ int linear_bwd_launch(unipool_ctx*, const LinearBwdArgs&, cudaStream_t);
 size_t linear_bwd_scratch(const unipool_ctx*, int T, int n_in, int n_out);
 int linear_fwd_tc(unipool_ctx*, const LinearArgs&, cudaStream_t);
 int linear_dx_tc(unipool_ctx*, const LinearBwdArgs&, const void* dp, cudaStream_t);
-int linear_dw_tc(unipool_ctx*, const LinearBwdArgs&, const void* dp, float* out, int splits, bool add, cudaStream_t);
-int linear_dw_splits_tc(const unipool_ctx*, int T, int n_in, int n_out);
+struct LinearDwPlan { int splits, dx_tile; };             // parts of the tokens; columns of the tiles of a launch with dx, 0: without
+LinearDwPlan linear_dw_plan_tc(const unipool_ctx*, int T, int n_in, int n_out, bool with_dx);
+int linear_dw_tc(unipool_ctx*, const LinearBwdArgs&, const void* dp, float* out, const LinearDwPlan&, bool add, cudaStream_t);
 int column_sum_launch(const float* parts, int n_parts, int64_t width, float* out, bool add, cudaStream_t);
 
 // grouped GEMMs: CUDA-core path (fp32 mode) and tcgen05 path (bf16 mode)

@@ -331,8 +331,8 @@ int dw_simt(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, float* out
 constexpr int kDyRows = 512;             // so few rows of dy are summed without a kernel of their own
 
 bool tensor_cores(const unipool_ctx* ctx) { return ctx->cfg.dtype == UNIPOOL_BF16; }
-int dw_splits(const unipool_ctx* ctx, int T, int n_in, int n_out) {
-  return tensor_cores(ctx) ? linear_dw_splits_tc(ctx, T, n_in, n_out) : dw_splits_simt(ctx, T, n_in, n_out);
+LinearDwPlan dw_plan(const unipool_ctx* ctx, int T, int n_in, int n_out, bool with_dx) {
+  return tensor_cores(ctx) ? linear_dw_plan_tc(ctx, T, n_in, n_out, with_dx) : LinearDwPlan{dw_splits_simt(ctx, T, n_in, n_out), 0};
 }
 
 template <typename E, int V, bool kFast>
@@ -366,16 +366,17 @@ int linear_launch(unipool_ctx* ctx, const LinearArgs& a, cudaStream_t s) {
   return rows_simt<kAlongK>(ctx, UNIPOOL_PH_LINEAR, p, s);
 }
 
-// Scratch: the parts of dW, then those of dbias.
-static size_t dw_parts(const unipool_ctx* ctx, int T, int n_in, int n_out) {
-  const int splits = dw_splits(ctx, T, n_in, n_out);
-  return splits > 1 ? (size_t)splits * n_in * n_out : 0;
-}
-size_t linear_bwd_scratch(const unipool_ctx* ctx, int T, int n_in, int n_out) {
+// Scratch: the parts of dbias, then those of dW.
+static size_t dw_parts(int splits, int n_in, int n_out) { return splits > 1 ? (size_t)splits * n_in * n_out : 0; }
+static size_t db_parts(const unipool_ctx* ctx, int T, int n_out) {
   int sums = 0;                                          // (the widest call: any activation, and in fp32 any alignment)
   for (const int act : {UNIPOOL_ACT_NONE, UNIPOOL_ACT_GELU})
     for (const int cols : {32 * (tensor_cores(ctx) ? 8 : 4), 32}) sums = std::max(sums, dp_row_blocks(ctx, T, n_out, cols, act));
-  return (dw_parts(ctx, T, n_in, n_out) + (sums > 1 ? (size_t)sums * n_out : 0)) * sizeof(float);
+  return sums > 1 ? (size_t)sums * n_out : 0;
+}
+size_t linear_bwd_scratch(const unipool_ctx* ctx, int T, int n_in, int n_out) {
+  const int splits = std::max(dw_plan(ctx, T, n_in, n_out, false).splits, dw_plan(ctx, T, n_in, n_out, true).splits);
+  return (db_parts(ctx, T, n_out) + dw_parts(splits, n_in, n_out)) * sizeof(float);
 }
 
 int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) {
@@ -391,15 +392,15 @@ int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) 
   // (few rows of dy itself are added up beside dW's parts: one launch less)
   const bool dy_rows = !act && a.dbias != nullptr && a.T <= kDyRows;
   if (act || (a.dbias != nullptr && !dy_rows)) {
-    float* parts = a.scratch ? a.scratch + dw_parts(ctx, a.T, a.n_in, a.n_out) : nullptr;
     int blocks = 1;
-    rc = tc ? dp_as<__nv_bfloat16, 8, true>(ctx, a, &blocks, parts, s)
-         : aligned16(a.dy, a.pre, act ? a.dp : nullptr) ? dp_as<float, 4, false>(ctx, a, &blocks, parts, s)
-                                                        : dp_as<float, 1, false>(ctx, a, &blocks, parts, s);
+    rc = tc ? dp_as<__nv_bfloat16, 8, true>(ctx, a, &blocks, a.scratch, s)
+         : aligned16(a.dy, a.pre, act ? a.dp : nullptr) ? dp_as<float, 4, false>(ctx, a, &blocks, a.scratch, s)
+                                                        : dp_as<float, 1, false>(ctx, a, &blocks, a.scratch, s);
     if (rc != UNIPOOL_OK) return rc;
-    if (a.dbias != nullptr && blocks > 1) db = {parts, blocks, a.n_out, a.dbias, !a.overwrite};
+    if (a.dbias != nullptr && blocks > 1) db = {a.scratch, blocks, a.n_out, a.dbias, !a.overwrite};
   }
-  if (a.dx != nullptr) {
+  const LinearDwPlan plan = a.dW != nullptr ? dw_plan(ctx, a.T, a.n_in, a.n_out, a.dx != nullptr) : LinearDwPlan{1, 0};
+  if (a.dx != nullptr && plan.dx_tile == 0) {
     if (tc) {
       rc = linear_dx_tc(ctx, a, dp, s);
     } else {
@@ -413,12 +414,12 @@ int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) 
     if (rc != UNIPOOL_OK) return rc;
   }
   if (a.dW != nullptr) {
-    const int splits = dw_splits(ctx, a.T, a.n_in, a.n_out);
-    float* out = splits > 1 ? a.scratch : a.dW;
+    const int splits = plan.splits;
+    float* out = splits > 1 ? a.scratch + db_parts(ctx, a.T, a.n_out) : a.dW;
     const bool add = splits == 1 && !a.overwrite;
-    rc = tc ? linear_dw_tc(ctx, a, dp, out, splits, add, s) : dw_simt(ctx, a, dp, out, splits, add, s);
+    rc = tc ? linear_dw_tc(ctx, a, dp, out, plan, add, s) : dw_simt(ctx, a, dp, out, splits, add, s);
     if (rc != UNIPOOL_OK) return rc;
-    if (splits > 1) dW = {a.scratch, splits, (int64_t)a.n_in * a.n_out, a.dW, !a.overwrite};
+    if (splits > 1) dW = {out, splits, (int64_t)a.n_in * a.n_out, a.dW, !a.overwrite};
   }
   if (dW.n == 0 && db.n == 0 && !dy_rows) return UNIPOOL_OK;
   PhaseTimer pt(ctx, UNIPOOL_PH_LINEAR_BWD, 1, s);

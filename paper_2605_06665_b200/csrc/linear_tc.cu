@@ -13,6 +13,7 @@
 // Bound by the tensor pipe (operands through shared memory; see expert_tc.cu) and, held for long, by power.
 #include <cuda.h>
 
+#include <algorithm>
 #include <type_traits>
 
 #include "common.cuh"
@@ -24,7 +25,7 @@ namespace unipool {
 
 namespace {
 
-enum LinearKind { kLinFwd, kLinFwd8, kLinDx, kLinDw };
+enum LinearKind { kLinFwd, kLinFwd8, kLinDx, kLinDw, kLinBoth };   // kLinBoth: dW's tiles, then dx's, in one launch
 
 constexpr uint32_t kLinHalf = 128 * 128;                 // 128 rows (columns) x 128 bytes of one operand
 constexpr uint32_t kLinBars = 229376;                    // operand stages and staging tiles fill this much
@@ -38,9 +39,12 @@ constexpr uint32_t kLinTile = 32 * kLinChunk * 2;        // a chunk of 32 rows i
 // added up in registers, where it is rounded to nearest.
 constexpr int kLinSegment = 12;                          // k-blocks of 64 tokens
 
-struct LinearParams {
+struct LinearGrid {
   int M, N;                          // rows and columns of the result
   int n_mt, n_nt, units, kb_total, kb_split;
+};
+struct LinearParams {
+  LinearGrid g, w;                   // w: of the weight gradient in kLinBoth
   int act;
   const float *bias, *x_scale, *w_scale;
   bool pre;                          // the value before the activation is stored too
@@ -48,12 +52,14 @@ struct LinearParams {
   const __nv_bfloat16* residual;     // [M, N] or NULL
   float* dw;                         // weight gradient: [splits, M, N]
   bool add;                          // ... +=
-  bool wide;                         // residual, or dw, is 32-byte aligned
+  bool wide, wide_dw;                // residual, and dw, are 32-byte aligned
   int32_t* status;
 };
 
+struct LinearMaps { CUtensorMap a, b, c, r, p, wa, wb; };  // operands, result, residual, value before the activation; kLinBoth: dW's operands
+
 struct LinearUnit { int mt, nt, split, kb0, kb1; };
-__device__ __forceinline__ LinearUnit linear_unit(const LinearParams& p, int u) {
+__device__ __forceinline__ LinearUnit linear_unit(const LinearGrid& p, int u) {
   LinearUnit t;
   const int per = p.n_mt * p.n_nt;
   t.split = u / per;
@@ -136,16 +142,15 @@ __device__ __forceinline__ void activate(float (&v)[32], int act) {
 // kN: columns of a tile, 256 or 128.
 template <int KIND, int kN, bool kRes, bool kPre>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
-linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB,
-                   const __grid_constant__ CUtensorMap tmC, const __grid_constant__ CUtensorMap tmR,
-                   const __grid_constant__ CUtensorMap tmP, LinearParams p) {
+linear_pair_kernel(const __grid_constant__ LinearMaps m, LinearParams p) {
   constexpr uint32_t kStage = kLinHalf + kN * 64;         // 128 rows of A, kN / 2 of B
   constexpr int kStages = KIND == kLinDw ? 7 : kN == 256 ? 6 : 8;
   constexpr uint32_t kStaging = KIND == kLinDw ? 0 : kLinTile;
   static_assert(kStages * kStage + kLinEpiWarps * kStaging == kLinBars, "shared memory");
   static_assert(kN == 256 || (kN == 128 && KIND != kLinDw), "columns of a tile");
+  constexpr bool kBoth = KIND == kLinBoth, kDw = KIND == kLinDw || kBoth;
   constexpr int kPart = kN / 4, kChunks = kPart / kLinChunk;   // columns of an epilogue warp, its chunks
-  constexpr bool kAMn = KIND == kLinDw, kBMn = KIND == kLinDx || KIND == kLinDw;
+  constexpr bool kBMn = KIND == kLinDx || kDw;
   constexpr int kKb = KIND == kLinFwd8 ? 128 : 64;       // elements of a k-block
   extern __shared__ uint8_t smem_raw[];
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~uintptr_t(1023));
@@ -169,8 +174,8 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       for (int i = 0; i < kLinEpiWarps; ++i) tc::mbar_init(&res_bar[i], 1);
     *abort = 0;
     tc::fence_barrier_init();
-    tc::tma_prefetch_desc(&tmA);
-    tc::tma_prefetch_desc(&tmB);
+    tc::tma_prefetch_desc(&m.a);
+    tc::tma_prefetch_desc(&m.b);
   }
   if (warp == 1) {
     tc::tmem_alloc_pair(tmem_ptr, 512);
@@ -182,6 +187,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   tc::tc_fence_after_sync();
   const uint32_t tmem_base = *tmem_ptr;
   grid_wait(p.bias, p.x_scale, p.w_scale, p.residual);
+  const int units = p.g.units + (kBoth ? p.w.units : 0);
+  auto is_dw = [&](int u) { return KIND == kLinDw || (kBoth && u < p.w.units); };
+  auto unit = [&](int u) { return kBoth ? (u < p.w.units ? linear_unit(p.w, u) : linear_unit(p.g, u - p.w.units)) : linear_unit(p.g, u); };
 
   if (warp == 0) {
     // ------------------------------------------------------------ TMA producer (one in each CTA)
@@ -189,17 +197,19 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       int stage = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int u = pair; u < p.units && ok; u += n_pairs) {
-        const LinearUnit t = linear_unit(p, u);
+      for (int u = pair; u < units && ok; u += n_pairs) {
+        const LinearUnit t = unit(u);
+        const bool dw = is_dw(u);
         for (int kb = t.kb0; kb < t.kb1; ++kb) {
           if (!tc::mbar_wait(&empty_bar[stage], phase ^ 1u, abort)) { linear_timeout(p.status, abort, 41); ok = false; break; }
           uint8_t* sA = smem + stage * kStage;
           uint8_t* sB = sA + kLinHalf;
           if (rank == 0) tc::mbar_expect_tx(&full_bar[stage], 2 * kStage);         // both CTAs' bytes
-          if constexpr (kAMn) tc::tma_load_3d_pair(sA, &tmA, &full_bar[stage], 0, kb * kKb, t.mt * 4 + rank * 2);
-          else tc::tma_load_2d_pair(sA, &tmA, &full_bar[stage], kb * kKb, t.mt * 256 + rank * 128);
-          if constexpr (kBMn) tc::tma_load_3d_pair(sB, &tmB, &full_bar[stage], 0, kb * kKb, (t.nt * 2 + rank) * (kN / 128));
-          else tc::tma_load_2d_pair(sB, &tmB, &full_bar[stage], kb * kKb, t.nt * kN + rank * (kN / 2));
+          const CUtensorMap *ma = kBoth && dw ? &m.wa : &m.a, *mb = kBoth && dw ? &m.wb : &m.b;
+          if (kDw && dw) tc::tma_load_3d_pair(sA, ma, &full_bar[stage], 0, kb * kKb, t.mt * 4 + rank * 2);
+          else tc::tma_load_2d_pair(sA, ma, &full_bar[stage], kb * kKb, t.mt * 256 + rank * 128);
+          if constexpr (kBMn) tc::tma_load_3d_pair(sB, mb, &full_bar[stage], 0, kb * kKb, (t.nt * 2 + rank) * (kN / 128));
+          else tc::tma_load_2d_pair(sB, mb, &full_bar[stage], kb * kKb, t.nt * kN + rank * (kN / 2));
           if (++stage == kStages) { stage = 0; phase ^= 1u; }
         }
       }
@@ -209,16 +219,18 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   } else if (warp == 1) {
     // ------------------------------------------------------------ MMA issuer (leader CTA only)
     if (lane == 0 && rank == 0) {
-      constexpr uint32_t idesc = KIND == kLinFwd8 ? tc::instr_desc_e4m3(kN, 256) : tc::instr_desc_bf16(kN, kAMn, kBMn, 256);
-      constexpr uint32_t a_lbo = kAMn ? kLinHalf / 2 : 16, b_lbo = kBMn ? kLinHalf / 2 : 16;
-      constexpr uint32_t a_step = (kAMn ? 16 * 128 : 32) >> 4, b_step = (kBMn ? 16 * 128 : 32) >> 4;
+      constexpr uint32_t b_lbo = kBMn ? kLinHalf / 2 : 16, b_step = (kBMn ? 16 * 128 : 32) >> 4;
       int stage = 0, local = 0;
       uint32_t phase = 0;
       bool ok = true;
-      for (int u = pair; u < p.units && ok; u += n_pairs) {
-        const LinearUnit t = linear_unit(p, u);
+      for (int u = pair; u < units && ok; u += n_pairs) {
+        const LinearUnit t = unit(u);
+        const bool dw = is_dw(u);
+        const bool a_mn = kDw && dw;
+        const uint32_t idesc = KIND == kLinFwd8 ? tc::instr_desc_e4m3(kN, 256) : tc::instr_desc_bf16(kN, a_mn, kBMn, 256);
+        const uint32_t a_lbo = a_mn ? kLinHalf / 2 : 16, a_step = (a_mn ? 16 * 128 : 32) >> 4;
         for (int kb = t.kb0; kb < t.kb1 && ok;) {
-          const int end = KIND == kLinDw ? min(t.kb1, kb + kLinSegment) : t.kb1;
+          const int end = a_mn ? min(t.kb1, kb + kLinSegment) : t.kb1;
           const int acc = local & 1;
           if (!tc::mbar_wait(&tmem_empty[acc], ((local >> 1) & 1) ^ 1u, abort)) { linear_timeout(p.status, abort, 42); ok = false; break; }
           ++local;
@@ -267,14 +279,16 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
       tc::tc_fence_after_sync();
       return got;
     };
-    for (int u = pair; u < p.units && ok; u += n_pairs) {
-      const LinearUnit t = linear_unit(p, u);
+    for (int u = pair; u < units && ok; u += n_pairs) {
+      const LinearUnit t = unit(u);
+      const bool dw = is_dw(u);
+      const LinearGrid& g = kBoth && dw ? p.w : p.g;
       const int row0 = t.mt * 256 + rank * 128 + quarter * 32, col0 = t.nt * kN + part * kPart;
-      const int nch = row0 < p.M ? max(0, min(kChunks, (p.N - col0) / kLinChunk)) : 0;
-      if constexpr (KIND == kLinDw) {
-        float sum[4][16];
+      const int nch = row0 < g.M ? max(0, min(kChunks, (g.N - col0) / kLinChunk)) : 0;
+      if (kDw && dw) {
+        float sum[kPart / 16][16];
 #pragma unroll
-        for (int q = 0; q < 4; ++q)
+        for (int q = 0; q < kPart / 16; ++q)
 #pragma unroll
           for (int i = 0; i < 16; ++i) sum[q][i] = 0.f;
 #pragma unroll 1
@@ -283,9 +297,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
           ok = wait_full(acc);
           if (!ok) break;
 #pragma unroll
-          for (int q = 0; q < 4; ++q) {
+          for (int q = 0; q < kPart / 16; ++q) {
             uint32_t rr[16];
-            tc::tmem_ld_32x16(tmem_base + lanes + acc * 256 + part * 64 + q * 16, rr);
+            tc::tmem_ld_32x16(tmem_base + lanes + acc * 256 + part * kPart + q * 16, rr);
             tc::tmem_ld_wait();
 #pragma unroll
             for (int i = 0; i < 16; ++i) sum[q][i] += __uint_as_float(rr[i]);
@@ -293,9 +307,9 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
           release(acc);
         }
         if (!ok) break;
-        float* out = &p.dw[((int64_t)t.split * p.M + row0 + lane) * p.N + col0];
+        float* out = &p.dw[((int64_t)t.split * g.M + row0 + lane) * g.N + col0];
 #pragma unroll
-        for (int ch = 0; ch < 2; ++ch) {
+        for (int ch = 0; ch < kChunks; ++ch) {
           if (ch >= nch) continue;                        // (row0 < M: then all of the warp's rows are, M being a multiple of 64)
 #pragma unroll
           for (int q = 0; q < 4; ++q) {
@@ -303,27 +317,28 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             float* o = out + ch * kLinChunk + 8 * q;
             uint32_t w[8];
             if (p.add) {
-              ld_sector(o, w, p.wide);
+              ld_sector(o, w, p.wide_dw);
 #pragma unroll
               for (int i = 0; i < 8; ++i) v[q % 2 * 8 + i] += __uint_as_float(w[i]);
             }
 #pragma unroll
             for (int i = 0; i < 8; ++i) w[i] = __float_as_uint(v[q % 2 * 8 + i]);
-            st_sector(o, w, p.wide);
+            st_sector(o, w, p.wide_dw);
           }
         }
-      } else {
+      }
+      if (KIND != kLinDw && !(kBoth && dw)) {
         const int acc = local & 1;
-        const bool mine = row0 + lane < p.M;
+        const bool mine = row0 + lane < g.M;
         uint32_t r1[16];
         if constexpr (kRes) {
           if (lane == 0 && nch > 0) {
             tc::bulk_wait_read<0>();                      // what last left from there
             tc::mbar_expect_tx(&res_bar[ew], kLinTile);
-            tc::tma_load_2d(stg, &tmR, &res_bar[ew], col0, row0);
+            tc::tma_load_2d(stg, &m.r, &res_bar[ew], col0, row0);
           }
           if (kChunks > 1 && mine && nch > 1) {
-            const __nv_bfloat16* r = p.residual + ((int64_t)(row0 + lane) * p.N + col0 + kLinChunk);
+            const __nv_bfloat16* r = p.residual + ((int64_t)(row0 + lane) * g.N + col0 + kLinChunk);
             ld_sector(r, r1, p.wide);
             ld_sector(r + 16, r1 + 8, p.wide);
           }
@@ -354,7 +369,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
             for (int i = 0; i < 32; ++i) v[i] *= xs * c.at(i);
           }
           if ((KIND == kLinFwd8 || (KIND == kLinFwd && kRes)) && p.bias != nullptr) c.load(p.bias + col, p.vec);
-          if (KIND != kLinDx && p.bias != nullptr) {
+          if (KIND != kLinDx && !kBoth && p.bias != nullptr) {
 #pragma unroll
             for (int i = 0; i < 32; ++i) v[i] += c.at(i);
           }
@@ -377,14 +392,14 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
               if (kPre) take();
             }
           }
-          if constexpr (KIND != kLinDx) {
+          if constexpr (KIND != kLinDx && !kBoth) {
             if (kPre || (!kRes && p.pre)) {               // leaves first, from the same tile
               if ((!kRes || ch == 1) && lane == 0) tc::bulk_wait_read<0>();
               __syncwarp();
               put_row(stg, lane, v);
               tc::fence_proxy_async();
               __syncwarp();
-              if (lane == 0) { tc::tma_store_2d(&tmP, stg, col, row0); tc::bulk_commit(); }
+              if (lane == 0) { tc::tma_store_2d(&m.p, stg, col, row0); tc::bulk_commit(); }
             }
             activate(v, p.act);
           }
@@ -402,7 +417,7 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
           put_row(stg, lane, v);
           tc::fence_proxy_async();
           __syncwarp();
-          if (lane == 0) { tc::tma_store_2d(&tmC, stg, col, row0); tc::bulk_commit(); }
+          if (lane == 0) { tc::tma_store_2d(&m.c, stg, col, row0); tc::bulk_commit(); }
         }
         if (!ok) break;
         if (nch == 0) release(acc);
@@ -423,25 +438,23 @@ linear_pair_kernel(const __grid_constant__ CUtensorMap tmA, const __grid_constan
   }
 }
 
-LinearParams linear_params(const unipool_ctx* ctx, int M, int N, int tile_n, int kb_total, int splits) {
-  LinearParams p{};
-  p.M = M; p.N = N;
-  p.n_mt = (M + 255) / 256; p.n_nt = (N + tile_n - 1) / tile_n;
-  p.kb_total = kb_total;
-  p.kb_split = (kb_total + splits - 1) / splits;
-  p.units = p.n_mt * p.n_nt * ((kb_total + p.kb_split - 1) / p.kb_split);
-  p.status = ctx->ws.status;
-  return p;
+LinearGrid linear_grid(int M, int N, int tile_n, int kb_total, int splits) {
+  LinearGrid g{};
+  g.M = M; g.N = N;
+  g.n_mt = (M + 255) / 256; g.n_nt = (N + tile_n - 1) / tile_n;
+  g.kb_total = kb_total;
+  g.kb_split = (kb_total + splits - 1) / splits;
+  g.units = g.n_mt * g.n_nt * ((kb_total + g.kb_split - 1) / g.kb_split);
+  return g;
 }
 
 template <int KIND, int kN, bool kRes, bool kPre>
-int launch_linear(unipool_ctx* ctx, int phase, const CUtensorMap& tmA, const CUtensorMap& tmB, const CUtensorMap& tmC,
-                  const CUtensorMap& tmR, const CUtensorMap& tmP, const LinearParams& p, cudaStream_t s) {
+int launch_linear(unipool_ctx* ctx, int phase, const LinearMaps& m, const LinearParams& p, cudaStream_t s) {
   PhaseTimer pt(ctx, phase, 1, s);
   auto kern = linear_pair_kernel<KIND, kN, kRes, kPre>;
   UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLinSmem));
-  const int pairs = ctx->sm_count / 2;
-  UP_KERNEL(kern, 2 * (p.units < pairs ? p.units : pairs), kLinThreads, kLinSmem, s, tmA, tmB, tmC, tmR, tmP, p);
+  const int pairs = ctx->sm_count / 2, units = p.g.units + p.w.units;
+  UP_KERNEL(kern, 2 * (units < pairs ? units : pairs), kLinThreads, kLinSmem, s, m, p);
   return UNIPOOL_OK;
 }
 
@@ -662,7 +675,9 @@ FewShape few_shape(int T, int M, int kb_total) {
 //   4096 -> 128   1 token 6.0/23.2/24.5   512 8.9/24.2/25.0   8000 19.6/25.6/25.5
 //   128 -> 4096   1 token 4.9/8.8/11.7    512 9.9/7.3/9.8     8000 82.3/47.0/46.7
 enum LinearForm { kFew, kPairs128, kPairs256 };
-LinearForm linear_form(const unipool_ctx* ctx, int M, int N, int kb, bool plain) {
+constexpr double kLaunchUs = 2.0;                        // from one kernel of a call to the next
+struct FormTime { LinearForm form; double us; };
+FormTime linear_form(const unipool_ctx* ctx, int M, int N, int kb, bool plain) {
   const int pairs = ctx->sm_count / 2;
   auto by_pairs = [&](int n, double busy, double alone, double rest) {
     const int64_t rounds = ((int64_t)((M + 255) / 256) * ((N + n - 1) / n) + pairs - 1) / pairs;
@@ -673,9 +688,9 @@ LinearForm linear_form(const unipool_ctx* ctx, int M, int N, int kb, bool plain)
     const FewShape f = few_shape(M, N, kb);
     const double ctas = (double)f.tiles * f.splits / ctx->sm_count, each = (kb + f.splits - 1) / f.splits * (16.0 + f.N / 8.0);
     const double few = 3.2 + 0.03 * f.N + (ctas > 1.0 ? 0.7 + ctas * each / 120.0 : each / 85.0);
-    if (ctas <= 2.0 && few < p128 && few < p256) return kFew;     // (several rounds of its CTAs never were the fastest)
+    if (ctas <= 2.0 && few < p128 && few < p256) return {kFew, few};     // (several rounds of its CTAs never were the fastest)
   }
-  return p128 < p256 ? kPairs128 : kPairs256;
+  return p128 < p256 ? FormTime{kPairs128, p128} : FormTime{kPairs256, p256};
 }
 
 template <int KIND>
@@ -729,81 +744,134 @@ static int linear_few_dx(unipool_ctx* ctx, const LinearBwdArgs& a, const void* d
 int linear_fwd_tc(unipool_ctx* ctx, const LinearArgs& a, cudaStream_t s) {
   const bool q8 = a.x_scale != nullptr;
   const int kb = q8 ? 128 : 64;
-  const LinearForm form = linear_form(ctx, a.T, a.n_out, (a.n_in + kb - 1) / kb, a.bias == nullptr && a.act == UNIPOOL_ACT_NONE);
+  const LinearForm form = linear_form(ctx, a.T, a.n_out, (a.n_in + kb - 1) / kb, a.bias == nullptr && a.act == UNIPOOL_ACT_NONE).form;
   if (form == kFew) return linear_few(ctx, a, s);
   const int tile_n = form == kPairs128 ? 128 : 256;
-  LinearParams p = linear_params(ctx, a.T, a.n_out, tile_n, (a.n_in + kb - 1) / kb, 1);
+  LinearParams p{};
+  p.g = linear_grid(a.T, a.n_out, tile_n, (a.n_in + kb - 1) / kb, 1);
+  p.status = ctx->ws.status;
   p.act = a.act;
   p.bias = a.bias; p.x_scale = a.x_scale; p.w_scale = a.w_scale;
   p.pre = a.pre != nullptr;
   p.vec = aligned(16, a.bias, a.w_scale);
   p.residual = static_cast<const __nv_bfloat16*>(a.residual);
   p.wide = aligned(32, a.residual);
-  CUtensorMap tmA, tmB, tmC, tmR, tmP;
+  LinearMaps m{};
   const MapKind kind = q8 ? kMapByteOperand : kMapOperand;
-  UP_TRY(map_2d(ctx, &tmA, a.x, a.n_in, a.T, kb, 128, kind));
-  UP_TRY(map_2d(ctx, &tmB, a.W, a.n_in, a.n_out, kb, tile_n / 2, kind));
-  UP_TRY(map_2d(ctx, &tmC, a.y, a.n_out, a.T, kLinChunk, 32, kMapBf16Chunk));
-  tmR = tmP = tmC;
-  if (a.residual != nullptr) UP_TRY(map_2d(ctx, &tmR, a.residual, a.n_out, a.T, kLinChunk, 32, kMapBf16Chunk));
-  if (a.pre != nullptr) UP_TRY(map_2d(ctx, &tmP, a.pre, a.n_out, a.T, kLinChunk, 32, kMapBf16Chunk));
+  UP_TRY(map_2d(ctx, &m.a, a.x, a.n_in, a.T, kb, 128, kind));
+  UP_TRY(map_2d(ctx, &m.b, a.W, a.n_in, a.n_out, kb, tile_n / 2, kind));
+  UP_TRY(map_2d(ctx, &m.c, a.y, a.n_out, a.T, kLinChunk, 32, kMapBf16Chunk));
+  if (a.residual != nullptr) UP_TRY(map_2d(ctx, &m.r, a.residual, a.n_out, a.T, kLinChunk, 32, kMapBf16Chunk));
+  if (a.pre != nullptr) UP_TRY(map_2d(ctx, &m.p, a.pre, a.n_out, a.T, kLinChunk, 32, kMapBf16Chunk));
   auto as = [&](auto n) {
     constexpr int N = decltype(n)::value;
     auto run = a.residual == nullptr ? (q8 ? launch_linear<kLinFwd8, N, false, false> : launch_linear<kLinFwd, N, false, false>)
                : a.pre == nullptr    ? (q8 ? launch_linear<kLinFwd8, N, true, false> : launch_linear<kLinFwd, N, true, false>)
                                      : (q8 ? launch_linear<kLinFwd8, N, true, true> : launch_linear<kLinFwd, N, true, true>);
-    return run(ctx, UNIPOOL_PH_LINEAR, tmA, tmB, tmC, tmR, tmP, p, s);
+    return run(ctx, UNIPOOL_PH_LINEAR, m, p, s);
   };
   return tile_n == 256 ? as(std::integral_constant<int, 256>()) : as(std::integral_constant<int, 128>());
 }
 
-int linear_dx_tc(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, cudaStream_t s) {
-  const LinearForm form = linear_form(ctx, a.T, a.n_in, a.n_out / 64, true);
-  if (form == kFew) return linear_few_dx(ctx, a, dp, s);
-  const int tile_n = form == kPairs128 ? 128 : 256;
-  LinearParams p = linear_params(ctx, a.T, a.n_in, tile_n, a.n_out / 64, 1);
+namespace {
+
+int dx_maps(unipool_ctx* ctx, LinearMaps& m, const LinearBwdArgs& a, const void* dp, int tile_n) {
+  UP_TRY(map_2d(ctx, &m.a, dp, a.n_out, a.T, 64, 128));
+  UP_TRY(map_mn(ctx, &m.b, a.W, a.n_in, a.n_out, tile_n / 128));
+  UP_TRY(map_2d(ctx, &m.c, a.dx, a.n_in, a.T, kLinChunk, 32, kMapBf16Chunk));
+  if (a.dx_residual != nullptr) UP_TRY(map_2d(ctx, &m.r, a.dx_residual, a.n_in, a.T, kLinChunk, 32, kMapBf16Chunk));
+  return UNIPOOL_OK;
+}
+int dw_maps(unipool_ctx* ctx, CUtensorMap& ma, CUtensorMap& mb, const LinearBwdArgs& a, const void* dp, int tile_n) {
+  UP_TRY(map_mn(ctx, &ma, dp, a.n_out, a.T, 2));
+  return map_mn(ctx, &mb, a.x, a.n_in, a.T, tile_n / 128);
+}
+LinearParams bwd_params(const unipool_ctx* ctx, const LinearBwdArgs& a, float* out, bool add) {
+  LinearParams p{};
+  p.status = ctx->ws.status;
   p.residual = static_cast<const __nv_bfloat16*>(a.dx_residual);
   p.wide = aligned(32, a.dx_residual);
-  CUtensorMap tmA, tmB, tmC, tmR;
-  UP_TRY(map_2d(ctx, &tmA, dp, a.n_out, a.T, 64, 128));
-  UP_TRY(map_mn(ctx, &tmB, a.W, a.n_in, a.n_out, tile_n / 128));
-  UP_TRY(map_2d(ctx, &tmC, a.dx, a.n_in, a.T, kLinChunk, 32, kMapBf16Chunk));
-  tmR = tmC;
-  if (a.dx_residual != nullptr) UP_TRY(map_2d(ctx, &tmR, a.dx_residual, a.n_in, a.T, kLinChunk, 32, kMapBf16Chunk));
+  p.add = add;
+  p.dw = out;
+  p.wide_dw = aligned(32, out);
+  return p;
+}
+
+}  // namespace
+
+int linear_dx_tc(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, cudaStream_t s) {
+  const LinearForm form = linear_form(ctx, a.T, a.n_in, a.n_out / 64, true).form;
+  if (form == kFew) return linear_few_dx(ctx, a, dp, s);
+  const int tile_n = form == kPairs128 ? 128 : 256;
+  LinearParams p = bwd_params(ctx, a, nullptr, false);
+  p.g = linear_grid(a.T, a.n_in, tile_n, a.n_out / 64, 1);
+  LinearMaps m{};
+  UP_TRY(dx_maps(ctx, m, a, dp, tile_n));
   auto as = [&](auto n) {
     constexpr int N = decltype(n)::value;
     auto run = a.dx_residual != nullptr ? launch_linear<kLinDx, N, true, false> : launch_linear<kLinDx, N, false, false>;
-    return run(ctx, UNIPOOL_PH_LINEAR_BWD, tmA, tmB, tmC, tmR, tmC, p, s);
+    return run(ctx, UNIPOOL_PH_LINEAR_BWD, m, p, s);
   };
   return tile_n == 256 ? as(std::integral_constant<int, 256>()) : as(std::integral_constant<int, 128>());
 }
 
-// Parts of the tokens that the weight gradient is taken in, so that its tiles fill the CTA pairs: the number with the least
-// time for its rounds of tiles (0.3 us a k-block) and for writing and reading the parts' sums (6 bytes a ns).
-int linear_dw_splits_tc(const unipool_ctx* ctx, int T, int n_in, int n_out) {
-  const int tiles = ((n_out + 255) / 256) * ((n_in + 255) / 256), kb = (T + 63) / 64, pairs = ctx->sm_count / 2;
-  int best = 1;
+// How the weight gradient is taken: the parts of the tokens, so that its tiles fill the CTA pairs, and whether dx's tiles go into the same
+// launch behind its own (short tiles after long ones).  Each by its time in us: rounds of tiles (0.3 us a k-block), the parts' sums
+// (6 bytes a ns written and read, and a launch), a launch between two kernels.
+LinearDwPlan linear_dw_plan_tc(const unipool_ctx* ctx, int T, int n_in, int n_out, bool with_dx) {
+  const int kb = (T + 63) / 64, pairs = ctx->sm_count / 2, kb_x = n_out / 64;
+  LinearDwPlan best{1, 0};
   double least = 0.0;
-  for (int splits = 1; splits <= 64 && splits <= kb; ++splits) {
-    const int len = (kb + splits - 1) / splits, parts = (kb + len - 1) / len;
-    if (parts != splits) continue;
-    const int rounds = (tiles * splits + pairs - 1) / pairs;
-    const double ns = rounds * (len * 300.0 + 1000.0) + (splits > 1 ? 3000.0 + 8.0 * splits * n_in * n_out / 6.0e3 : 0.0);
-    if (splits == 1 || ns < least) { best = splits; least = ns; }
+  const double apart = with_dx ? linear_form(ctx, T, n_in, kb_x, true).us + kLaunchUs + 3.3 : 0.0;
+  auto consider = [&](int tile, bool together) {
+    const int tiles = ((n_out + 255) / 256) * ((n_in + tile - 1) / tile), units_x = together ? ((T + 255) / 256) * ((n_in + tile - 1) / tile) : 0;
+    const double end = tile == 256 ? 3.5 : 2.0;
+    for (int splits = 1; splits <= 64 && splits <= kb && (splits == 1 || tiles * (splits - 1) < 2 * pairs); ++splits) {
+      const int len = (kb + splits - 1) / splits, parts = (kb + len - 1) / len;
+      if (parts != splits) continue;
+      // pair q takes units q, q + pairs, ...; the last to end is the first of one of these
+      const int units_w = tiles * splits, all = units_w + units_x;
+      double us = 0.0;
+      for (const int q : {0, units_w % pairs, all % pairs}) {
+        const int n = (all - q + pairs - 1) / pairs, w = q < units_w ? (units_w - q + pairs - 1) / pairs : 0;
+        const double busy = ((double)units_w * len + (double)units_x * kb_x) / ((double)pairs * (w * len + (n - w) * kb_x));
+        const double each = 0.29 + 0.09 * std::min(1.0, busy * busy);
+        us = std::max(us, w * std::max(len * each + 1.0, end) + (n - w) * std::max(kb_x * each + 1.0, end));
+      }
+      us += together ? (tile == 256 ? 6.3 : 4.4) : with_dx ? apart : 0.0;
+      if (splits > 1) us += 3.0 + 8.0 * splits * n_in * n_out / 6.0e6;
+      if (least == 0.0 || us < least) { best = {splits, together ? tile : 0}; least = us; }
+    }
+  };
+  consider(256, false);
+  if (with_dx) {
+    consider(128, true);
+    consider(256, true);
   }
   return best;
 }
 
 // out [splits, n_out, n_in]: the parts' sums, or with one part the gradient.
-int linear_dw_tc(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, float* out, int splits, bool add, cudaStream_t s) {
-  LinearParams p = linear_params(ctx, a.n_out, a.n_in, 256, (a.T + 63) / 64, splits);
-  p.add = add;
-  p.dw = out;
-  p.wide = aligned(32, out);
-  CUtensorMap tmA, tmB;
-  UP_TRY(map_mn(ctx, &tmA, dp, a.n_out, a.T, 2));
-  UP_TRY(map_mn(ctx, &tmB, a.x, a.n_in, a.T, 2));
-  return launch_linear<kLinDw, 256, false, false>(ctx, UNIPOOL_PH_LINEAR_BWD, tmA, tmB, tmA, tmA, tmA, p, s);
+int linear_dw_tc(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, float* out, const LinearDwPlan& plan, bool add, cudaStream_t s) {
+  const int kb = (a.T + 63) / 64, tile_n = plan.dx_tile == 128 ? 128 : 256;
+  LinearParams p = bwd_params(ctx, a, out, add);
+  LinearMaps m{};
+  const LinearGrid w = linear_grid(a.n_out, a.n_in, tile_n, kb, plan.splits);
+  if (plan.dx_tile == 0) {
+    p.g = w;
+    UP_TRY(dw_maps(ctx, m.a, m.b, a, dp, tile_n));
+    return launch_linear<kLinDw, 256, false, false>(ctx, UNIPOOL_PH_LINEAR_BWD, m, p, s);
+  }
+  p.w = w;
+  p.g = linear_grid(a.T, a.n_in, tile_n, a.n_out / 64, 1);
+  UP_TRY(dx_maps(ctx, m, a, dp, tile_n));
+  UP_TRY(dw_maps(ctx, m.wa, m.wb, a, dp, tile_n));
+  auto as = [&](auto n) {
+    constexpr int N = decltype(n)::value;
+    auto run = a.dx_residual != nullptr ? launch_linear<kLinBoth, N, true, false> : launch_linear<kLinBoth, N, false, false>;
+    return run(ctx, UNIPOOL_PH_LINEAR_BWD, m, p, s);
+  };
+  return tile_n == 256 ? as(std::integral_constant<int, 256>()) : as(std::integral_constant<int, 128>());
 }
 
 }  // namespace unipool

@@ -210,7 +210,7 @@ template <int R> __device__ __forceinline__ int row_of_lane(int lane) { return l
 // row lay in every warp's registers and had to be added up at the end: 16384 rows of 768 bf16 22.5 us instead of 18.7.)
 // kRing: R rows are one run of bytes in memory; runs are copied, from the 16-byte boundary below to the one above, into a ring in
 // shared memory some stages ahead, so that reads go on while rows are worked on and whatever the rows' alignment (16384 rows of
-// 770 bf16 read element by element 69 us, through the ring 37).  Without it (arrays off 16 bytes, rows too long for two stages) the loads go
+// 770 bf16 read element by element 69 us, through the ring 35).  Without it (arrays off 16 bytes, rows too long for two stages) the loads go
 // from memory into registers.
 // The sums' order depends on the sizes alone.
 template <typename E, int V, int VPT, int R, bool kRing>

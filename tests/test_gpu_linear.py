@@ -285,12 +285,39 @@ def test_backward_sizes(train, T, n_in, n_out):
     torch.cuda.synchronize()
     assert untouched(xw, dx) and untouched(ww, dW) and untouched(bw, db)
     check_backward(m, d, T, "relu", dx, dW, db)
-    # one at a time, the same bits; added to what is there
+    # once more, the same bits; added to what is there
     dx2, dW2, db2 = torch.empty_like(dx), torch.full_like(dW, 2.0), torch.full_like(db, 2.0)
-    call_backward(m, d, T, n_in, n_out, "relu", dx2, None, None)
-    call_backward(m, d, T, n_in, n_out, "relu", None, dW2, None, flags=0)
-    call_backward(m, d, T, n_in, n_out, "relu", None, None, db2, flags=0)
+    call_backward(m, d, T, n_in, n_out, "relu", dx2, dW2, db2, flags=0)
     assert torch.equal(dx2, dx) and torch.equal(dW2, dW + 2.0) and torch.equal(db2, db + 2.0)
+    # one at a time (in one launch the products may be cut into other parts than alone)
+    call_backward(m, d, T, n_in, n_out, "relu", dx2, None, None)
+    call_backward(m, d, T, n_in, n_out, "relu", None, dW2, None)
+    call_backward(m, d, T, n_in, n_out, "relu", None, None, db2)
+    check_backward(m, d, T, "relu", dx2, dW2, db2)
+    dW3, db3 = torch.full_like(dW, 2.0), torch.full_like(db, 2.0)
+    call_backward(m, d, T, n_in, n_out, "relu", None, dW3, None, flags=0)
+    call_backward(m, d, T, n_in, n_out, "relu", None, None, db3, flags=0)
+    assert torch.equal(dW3, dW2 + 2.0) and torch.equal(db3, db2 + 2.0)
+
+
+@pytest.mark.parametrize("residual", [False, True])
+@pytest.mark.parametrize("T,n_in,n_out", [(129, 832, 448), (600, 3008, 640), (1501, 832, 2048), (2500, 1600, 704), (4111, 1088, 1536),
+                                          (6001, 512, 1984), (7003, 704, 704)])
+def test_backward_products_of_one_launch(train, T, n_in, n_out, residual):
+    """Sizes at which dx and dW share a launch in bf16: both tile widths, ragged in each direction, dW in one part and in several."""
+    m = train
+    d = backward_case(m, T, n_in, n_out, "relu", seed=5)
+    xw, dx = guarded((T, n_in), m.dt)
+    ww, dW = guarded((n_out, n_in), torch.float32)
+    db = torch.empty(n_out, device="cuda")
+    d = d if residual else dict(d, res=None)
+    call_backward(m, d, T, n_in, n_out, "relu", dx, dW, db)
+    torch.cuda.synchronize()
+    assert untouched(xw, dx) and untouched(ww, dW)
+    check_backward(m, d, T, "relu", dx, dW, db)
+    dx2, dW2 = (d["res"].clone() if residual else torch.empty_like(dx)), torch.full_like(dW, 2.0)
+    call_backward(m, d, T, n_in, n_out, "relu", dx2, dW2, None, flags=0, res=dx2 if residual else None)   # dx onto its residual
+    assert torch.equal(dx2, dx) and torch.equal(dW2, dW + 2.0)
 
 
 @pytest.mark.parametrize("act", ACTS)
