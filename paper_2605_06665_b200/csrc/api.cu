@@ -431,7 +431,7 @@ int unipool_rmsnorm(unipool_ctx* ctx, const void* x, const void* y, int32_t T, i
 }
 
 size_t unipool_rmsnorm_bwd_scratch(const unipool_ctx* ctx, int32_t T, int32_t width) {
-  return ctx == nullptr || T < 1 || width < 1 ? 0 : rmsnorm_bwd_scratch(ctx, T, width);
+  return ctx == nullptr || T < 1 || width < 1 || width > kNormMaxWidth ? 0 : rmsnorm_bwd_scratch(ctx, T, width);
 }
 
 int unipool_rmsnorm_bwd(unipool_ctx* ctx, const void* dh, const void* r, int32_t T, int32_t width, const float* w,
@@ -488,7 +488,8 @@ int unipool_linear_scaled(unipool_ctx* ctx, const uint8_t* x, const float* x_sca
 }
 
 size_t unipool_linear_bwd_scratch(const unipool_ctx* ctx, int32_t T, int32_t n_in, int32_t n_out) {
-  if (ctx == nullptr || T < 1 || n_in < 64 || n_out < 64 || n_in % 64 != 0 || n_out % 64 != 0) return 0;
+  const auto features = [](int32_t n) { return n >= 64 && n <= (1 << 21) && n % 64 == 0; };
+  if (ctx == nullptr || T < 1 || !features(n_in) || !features(n_out)) return 0;
   return linear_bwd_scratch(ctx, T, n_in, n_out);
 }
 
@@ -502,7 +503,10 @@ int unipool_linear_bwd(unipool_ctx* ctx, const void* dy, int32_t T, int32_t n_ou
   UP_REQUIRE((flags & ~UNIPOOL_WGRAD_OVERWRITE) == 0, UNIPOOL_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
   if (dx != nullptr) CHECK_PTR(W);
   if (dW != nullptr) CHECK_PTR(x);
-  if ((dW != nullptr || dbias != nullptr) && T > 0 && linear_bwd_scratch(ctx, T, n_in, n_out) > 0) CHECK_SCRATCH(scratch);
+  // (its size, which takes a search, only where it decides)
+  if ((dW != nullptr || dbias != nullptr) && T > 0 && (scratch == nullptr || (reinterpret_cast<uintptr_t>(scratch) & 15) != 0) &&
+      linear_bwd_scratch(ctx, T, n_in, n_out) > 0)
+    CHECK_SCRATCH(scratch);
   CHECK_ALIGNED(ctx, dy); CHECK_ALIGNED(ctx, pre); CHECK_ALIGNED(ctx, dp); CHECK_ALIGNED(ctx, x); CHECK_ALIGNED(ctx, W);
   CHECK_ALIGNED(ctx, dx_residual); CHECK_ALIGNED(ctx, dx); CHECK_ALIGNED(ctx, dW);
   LinearBwdArgs a{dy, pre, x, W, T, n_in, n_out, act, dp, dx_residual, dx, dW, dbias, static_cast<float*>(scratch),

@@ -434,8 +434,9 @@ NormBwdShape norm_bwd_shape_of(const unipool_ctx* ctx, int T, int width, int v, 
   }
   s.smem = s.stages > 0 ? (uint32_t)(s.stages * stage + 64) : 0;
   // (few rows on one block: no sums to add up behind it, which costs as much as three steps of a block)
-  const int all = (T + s.rows - 1) / s.rows, most = ctx->sm_count * per_sm;
-  s.blocks = all <= 4 ? 1 : all < most ? all : most;
+  const int64_t all = ((int64_t)T + s.rows - 1) / s.rows;
+  const int most = ctx->sm_count * per_sm;
+  s.blocks = all <= 4 ? 1 : all < most ? (int)all : most;
   return s;
 }
 NormBwdShape norm_bwd_shape(const unipool_ctx* ctx, int T, int width, bool aligned, int arrays) {

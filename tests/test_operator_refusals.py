@@ -155,6 +155,9 @@ def test_linear_backward(lib, ctx):
 def test_scratch_sizes_of_nothing(lib, ctx):
     assert lib.unipool_rmsnorm_bwd_scratch(None, 10, 768) == 0 and lib.unipool_rmsnorm_bwd_scratch(ctx, 0, 768) == 0
     assert lib.unipool_linear_bwd_scratch(None, 10, 64, 64) == 0 and lib.unipool_linear_bwd_scratch(ctx, 10, 65, 64) == 0
+    # beyond what the calls take
+    assert lib.unipool_rmsnorm_bwd_scratch(ctx, 10, 16384) == 64 and lib.unipool_rmsnorm_bwd_scratch(ctx, 10, 16385) == 0
+    assert lib.unipool_linear_bwd_scratch(ctx, 10, 64, 1 << 21) == 64 and lib.unipool_linear_bwd_scratch(ctx, 10, 64, (1 << 21) + 64) == 0
 
 
 def test_another_device_is_current(lib, ctx):
