@@ -471,7 +471,7 @@ template <typename... P> bool aligned(uintptr_t n, P... p) { return ((... | rein
 // share a tile's contraction and add up through each other's shared memory, in the order of their ranks; each then finishes every
 // S-th token.  Bound by the weights' bytes and, below some megabytes of them, by latency: every CTA asks for all of its weights
 // at once as far as they fit its stages.
-constexpr int kFewTokens = 128, kFewMaxStages = 12, kFewThreads = 192;
+constexpr int kFewTokens = 128, kFewMaxStages = 12;
 constexpr uint32_t kFewBars = 512;
 
 struct FewParams {
@@ -494,8 +494,9 @@ __device__ __forceinline__ void store_bf16x4(__nv_bfloat16* p, const float (&v)[
   *reinterpret_cast<uint2*>(p) = make_uint2(tc::pack_bf16(v[0], v[1]), tc::pack_bf16(v[2], v[3]));
 }
 
-template <int KIND, int S>
-__global__ void __cluster_dims__(S, 1, 1) __launch_bounds__(kFewThreads)
+// E epilogue warps: four or sixteen (few_shape).
+template <int KIND, int S, int E>
+__global__ void __cluster_dims__(S, 1, 1) __launch_bounds__(64 + 32 * E)
 linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant__ CUtensorMap tmX, FewParams p) {
   constexpr bool kAMn = KIND == kLinDx;
   constexpr int kKb = KIND == kLinFwd8 ? 128 : 64;
@@ -586,7 +587,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       if (!some && lane == 0) linear_timeout(p.status, abort, 53);
       tc::tc_fence_after_sync();
     }
-    for (int c = 0; c < p.N; c += 16) {
+    for (int c = (warp - 2) / 4 * 16; c < p.N; c += E * 4) {
       uint32_t rr[16];
       if (some) {
         tc::tmem_ld_32x16(tmem + (static_cast<uint32_t>(quarter * 32) << 16) + c, rr);
@@ -599,7 +600,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   }
   if constexpr (S > 1) tc::cluster_sync(); else __syncthreads();   // every CTA's sums are there
 
-  // Four features to a lane, a token to a warp: of the cluster's 6 S warps each takes every 6 S-th token.
+  // Four features to a lane, a token to a warp: of the cluster's (2 + E) S warps each takes every (2 + E) S-th token.
   const int m = m0 + 4 * lane;
   if (m < p.M) {
     float4 b = make_float4(0.f, 0.f, 0.f, 0.f), ws = b;
@@ -608,7 +609,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     if (KIND == kLinFwd8)
       ws = make_float4(__ldg(p.w_scale + m), __ldg(p.w_scale + m + 1), __ldg(p.w_scale + m + 2), __ldg(p.w_scale + m + 3));
     const uint32_t mine = tc::smem_u32(sums) + lane * 16;
-    constexpr int kWarps = kFewThreads / 32;
+    constexpr int kWarps = 2 + E;
 #pragma unroll 2
     for (int t = rank * kWarps + warp; t < p.N && t0 + t < p.T; t += S * kWarps) {
       const int64_t at = (int64_t)(t0 + t) * p.M + m;
@@ -642,26 +643,29 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
   }
 }
 
-template <int KIND, int S>
+template <int KIND, int S, int E>
 int launch_few(unipool_ctx* ctx, int phase, const CUtensorMap& tmW, const CUtensorMap& tmX, const FewParams& p, uint32_t smem,
                cudaStream_t s) {
   PhaseTimer pt(ctx, phase, 1, s);
-  auto kern = linear_few_kernel<KIND, S>;
+  auto kern = linear_few_kernel<KIND, S, E>;
   UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 232448));
-  UP_KERNEL(kern, dim3((p.M + 127) / 128 * S, (p.T + p.N - 1) / p.N), kFewThreads, smem, s, tmW, tmX, p);
+  UP_KERNEL(kern, dim3((p.M + 127) / 128 * S, (p.T + p.N - 1) / p.N), 64 + 32 * E, smem, s, tmW, tmX, p);
   return UNIPOOL_OK;
 }
 
 // How a call runs on the kernel for few tokens: a cluster of eight or four lies inside one GPC of 16 to 18 SMs, so that with two
 // CTAs on an SM 32 clusters of eight run at a time, 64 of four, 144 of two, and half as many with one (one more than that, and the
 // last come second: 384 tokens, 4096 -> 1536 on 36 clusters 19 us instead of 12).
-struct FewShape { int N, tiles, splits; bool half; };      // half: two CTAs share an SM's memory
+struct FewShape { int N, tiles, splits; bool half, wide; };   // half: two CTAs share an SM's memory; wide: sixteen epilogue warps
 FewShape few_shape(int T, int M, int kb_total) {
   FewShape f;
   f.N = T < kFewTokens ? (T + 15) / 16 * 16 : kFewTokens;
   f.tiles = (int)((int64_t)((M + 127) / 128) * ((T + f.N - 1) / f.N));
   f.splits = f.tiles <= 28 ? 8 : f.tiles <= 60 ? 4 : f.tiles <= 140 ? 2 : 1;
   while (f.splits > kb_total) f.splits /= 2;
+  // (each CTA finishes its share of the tokens in rounds of as many as it has warps, some 0.35 us each: 128 -> 4096, 128 tokens 8.3 us with
+  // four epilogue warps and 6.4 with sixteen; where a cluster of eight shares them, 9.2 and 10.0)
+  f.wide = f.N > 32 && f.splits <= 2;
   f.half = f.tiles > (f.splits == 8 ? 16 : f.splits == 4 ? 32 : f.splits == 2 ? 72 : 148);
   return f;
 }
@@ -670,10 +674,10 @@ FewShape few_shape(int T, int M, int kb_total) {
 // tiles, 0.29 to 0.38 us a k-block (what shared memory moves; less while half the chip is idle), a start and an end.  The kernel
 // for few tokens: the bytes that its CTAs bring into an SM (85 a ns for one, 120 for two), and adding up.  Measured in us, few
 // tokens / 128 columns / 256 columns, bf16 with a residual:
-//   768 -> 2048   1 token 4.8/9.1/11.3    128 9.0/9.9/12.4    512 9.8/10.0/12.5    2048 14.4/15.5/13.3   8000 62.8/39.0/31.6
-//   4096 -> 1536  1 token 5.9/23.4/25.7   128 9.3/24.2/26.8   512 14.5/24.6/27.0   1501 30.7/27.0/27.7   8000 120/122/78
+//   768 -> 2048   1 token 5.1/9.3/11.5    128 9.2/10.1/12.7   512 8.3/10.5/12.8   2048 13.5/15.2/13.5   8000 60/39/32
+//   4096 -> 1536  1 token 6.1/23.7/26.0   128 9.7/24.5/27.2   512 15.0/24.9/27.4  1501 27.9/26.0/28.7   8000 120/122/78
 //   4096 -> 128   1 token 6.0/23.2/24.5   512 8.9/24.2/25.0   8000 19.6/25.6/25.5
-//   128 -> 4096   1 token 4.9/8.8/11.7    512 9.9/7.3/9.8     8000 82.3/47.0/46.7
+//   128 -> 4096   1 token 3.9/6.6/8.8     512 8.9/7.6/10.2    8000 80/47/47
 enum LinearForm { kFew, kPairs128, kPairs256 };
 constexpr double kLaunchUs = 2.0;                        // from one kernel of a call to the next
 struct FormTime { LinearForm form; double us; };
@@ -687,7 +691,7 @@ FormTime linear_form(const unipool_ctx* ctx, int M, int N, int kb, bool plain) {
   if (M <= 16 * 1024) {
     const FewShape f = few_shape(M, N, kb);
     const double ctas = (double)f.tiles * f.splits / ctx->sm_count, each = (kb + f.splits - 1) / f.splits * (16.0 + f.N / 8.0);
-    const double few = 3.2 + 0.03 * f.N + (ctas > 1.0 ? 0.7 + ctas * each / 120.0 : each / 85.0);
+    const double few = 3.2 + (f.wide ? 0.02 : 0.03) * f.N + (ctas > 1.0 ? 1.7 + ctas * each / 120.0 : each / 85.0);
     if (ctas <= 2.0 && few < p128 && few < p256) return {kFew, few};     // (several rounds of its CTAs never were the fastest)
   }
   return p128 < p256 ? FormTime{kPairs128, p128} : FormTime{kPairs256, p256};
@@ -702,8 +706,12 @@ int few_as(unipool_ctx* ctx, int phase, const CUtensorMap& tmW, const CUtensorMa
   p.stages = most < kFewMaxStages ? most : kFewMaxStages;
   if (p.stages > need) p.stages = need;
   const uint32_t bytes = p.stages * stage > p.N * 512u ? p.stages * stage : p.N * 512u;   // the sums lie there too
-  auto run = splits == 8 ? launch_few<KIND, 8> : splits == 4 ? launch_few<KIND, 4> : splits == 2 ? launch_few<KIND, 2> : launch_few<KIND, 1>;
-  return run(ctx, phase, tmW, tmX, p, 2048 + bytes, s);
+  auto as = [&](auto e) {
+    constexpr int E = decltype(e)::value;
+    auto run = splits == 8 ? launch_few<KIND, 8, E> : splits == 4 ? launch_few<KIND, 4, E> : splits == 2 ? launch_few<KIND, 2, E> : launch_few<KIND, 1, E>;
+    return run(ctx, phase, tmW, tmX, p, 2048 + bytes, s);
+  };
+  return f.wide ? as(std::integral_constant<int, 16>()) : as(std::integral_constant<int, 4>());
 }
 
 }  // namespace
