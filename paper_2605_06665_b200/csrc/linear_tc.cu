@@ -674,10 +674,10 @@ FewShape few_shape(int T, int M, int kb_total) {
 // tiles, 0.29 to 0.38 us a k-block (what shared memory moves; less while half the chip is idle), a start and an end.  The kernel
 // for few tokens: the bytes that its CTAs bring into an SM (85 a ns for one, 120 for two), and adding up.  Measured in us, few
 // tokens / 128 columns / 256 columns, bf16 with a residual:
-//   768 -> 2048   1 token 5.1/9.3/11.5    128 9.2/10.1/12.7   512 8.3/10.5/12.8   2048 13.5/15.2/13.5   8000 60/39/32
-//   4096 -> 1536  1 token 6.1/23.7/26.0   128 9.7/24.5/27.2   512 15.0/24.9/27.4  1501 27.9/26.0/28.7   8000 120/122/78
-//   4096 -> 128   1 token 6.0/23.2/24.5   512 8.9/24.2/25.0   8000 19.6/25.6/25.5
-//   128 -> 4096   1 token 3.9/6.6/8.8     512 8.9/7.6/10.2    8000 80/47/47
+//   768 -> 2048   1 token 5.1/9.3/11.5    128 9.2/10.1/12.7   512 8.3/10.5/12.8   2048 13.5/15.2/13.5   8000 47.7/38.3/31.4
+//   4096 -> 1536  1 token 6.1/23.7/26.0   128 9.7/24.5/27.2   512 15.0/24.9/27.4  1501 27.9/26.0/28.7   8000 105/123/79
+//   4096 -> 128   1 token 6.0/23.2/24.5   512 8.9/24.2/25.0   8000 18.3/25.3/27.1
+//   128 -> 4096   1 token 3.9/6.6/8.8     512 8.9/7.6/10.2    8000 66.3/47.8/47.5
 enum LinearForm { kFew, kPairs128, kPairs256 };
 constexpr double kLaunchUs = 2.0;                        // from one kernel of a call to the next
 struct FormTime { LinearForm form; double us; };
