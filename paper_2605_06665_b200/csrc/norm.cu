@@ -10,6 +10,7 @@
 // columns), four or sixteen warps beyond; all of a thread's loads are issued before the first is used.  Rows whose bytes are no
 // multiple of 16, and misaligned tensors, go element by element through the same kernels.
 // Sums of squares, the statistics and the gradient of w are fp32; h is formed from the unrounded sum r.
+#include <cooperative_groups.h>
 #include <cuda_fp8.h>
 
 #include <type_traits>
@@ -212,9 +213,10 @@ template <int R> __device__ __forceinline__ int row_of_lane(int lane) { return l
 // shared memory some stages ahead, so that reads go on while rows are worked on and whatever the rows' alignment (16384 rows of
 // 770 bf16 read element by element 69 us, through the ring 35).  Without it (arrays off 16 bytes, rows too long for two stages) the loads go
 // from memory into registers.
-// The sums' order depends on the sizes alone.
-template <typename E, int V, int VPT, int R, bool kRing>
-__global__ void __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_kernel(NormBwdParams p) {
+// The sums' order depends on the sizes alone.  C > 1: the blocks are one cluster, which adds its sums for dw up through each other's shared
+// memory, in the order of the ranks.
+template <typename E, int V, int VPT, int R, bool kRing, int C>
+__global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_kernel(NormBwdParams p) {
   extern __shared__ __align__(128) uint8_t ring[];       // [stages][dh, r, dr][R rows], then the barriers
   __shared__ float part[2][16][R];
   __shared__ int abort_word;
@@ -399,19 +401,36 @@ __global__ void __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_
   if (kRing && *abort)
     for (int i = 0; i < 200; ++i) __nanosleep(1000);     // let copies already in flight land before the block retires
   if (p.dw == nullptr) return;
-  float* out = &p.dw[(int64_t)blockIdx.x * p.width];
+  float* out = C > 1 ? reinterpret_cast<float*>(ring) : &p.dw[(int64_t)blockIdx.x * p.width];
+  const bool add = C == 1 && p.add;
+  if (C > 1) __syncthreads();                            // (the rows in the ring are worked on)
 #pragma unroll
   for (int i = 0; i < VPT; ++i) {
     const int c = column(i);
     if (c >= p.width) continue;
 #pragma unroll
-    for (int j = 0; j < V; ++j) out[c + j] = p.add ? out[c + j] + dw[i][j] : dw[i][j];
+    for (int j = 0; j < V; ++j) out[c + j] = add ? out[c + j] + dw[i][j] : dw[i][j];
+  }
+  if constexpr (C > 1) {
+    namespace cg = cooperative_groups;
+    cg::cluster_group cluster = cg::this_cluster();
+    cluster.sync();
+    const int each = (p.width + C - 1) / C, c0 = (int)blockIdx.x * each, c1 = min(p.width, c0 + each);
+    for (int c = c0 + t; c < c1; c += blockDim.x) {
+      float v = cluster.map_shared_rank(out, 0)[c];
+#pragma unroll
+      for (int q = 1; q < C; ++q) v += cluster.map_shared_rank(out, q)[c];
+      float* o = &p.dw[c];
+      *o = p.add ? *o + v : v;
+    }
+    cluster.sync();                                      // no block leaves while another reads its sums
   }
 }
 
 // How the backward kernel runs: elements of a vector, vectors of a thread, threads and rows of a block, blocks, stages of the ring
-// (0: none) and its bytes.
-struct NormBwdShape { int v, vpt, threads, rows, blocks, stages; uint32_t smem; };
+// (0: none) and its bytes; whether with dw a cluster takes the rows instead.
+constexpr int kNormBwdCluster = 8;
+struct NormBwdShape { int v, vpt, threads, rows, blocks, stages; uint32_t smem; bool cluster; };
 constexpr int norm_bwd_rows(int V, int bytes, int vpt) {   // 48 registers of elements, 24 of narrower vectors
   return V * bytes == 16 ? (vpt >= 4 ? 1 : 4 / vpt) : vpt >= 8 ? 1 : 8 / (vpt * (V * bytes == 8 ? 2 : 1));
 }
@@ -437,6 +456,9 @@ NormBwdShape norm_bwd_shape_of(const unipool_ctx* ctx, int T, int width, int v, 
   const int64_t all = ((int64_t)T + s.rows - 1) / s.rows;
   const int most = ctx->sm_count * per_sm;
   s.blocks = all <= 4 ? 1 : all < most ? (int)all : most;
+  // (some more on a cluster of eight: a step or two of its blocks, but no launch behind them and no scratch, 4.5 us of the host's time.  48 rows
+  // of 768 bf16 5.0 us on a cluster and 4.5 in two launches, 96 rows 6.2 and 4.5)
+  s.cluster = all > 4 && all <= (s.rows > 1 ? 2 : 1) * kNormBwdCluster && s.vpt <= 8;
   return s;
 }
 NormBwdShape norm_bwd_shape(const unipool_ctx* ctx, int T, int width, bool aligned, int arrays) {
@@ -491,17 +513,23 @@ template <bool kNorm, typename E> int norm_as(unipool_ctx* ctx, const NormParams
 
 template <typename E, int V, int VPT, bool kRing>
 int norm_bwd_run(const NormBwdShape& f, const NormBwdParams& p, cudaStream_t s) {
-  auto kern = rmsnorm_bwd_kernel<E, V, VPT, norm_bwd_rows(V, (int)sizeof(E), VPT), kRing>;
-  if (kRing) UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 223 * 1024));
-  UP_KERNEL(kern, f.blocks, f.threads, f.smem, s, p);
-  return UNIPOOL_OK;
+  auto run = [&](auto c) {
+    constexpr int C = decltype(c)::value;
+    auto kern = rmsnorm_bwd_kernel<E, V, VPT, norm_bwd_rows(V, (int)sizeof(E), VPT), kRing, C>;
+    const uint32_t sums = C > 1 ? p.width * 4u : 0u;     // they lie where the ring was
+    if (kRing || C > 1) UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, 223 * 1024));
+    UP_KERNEL(kern, C > 1 ? C : f.blocks, f.threads, f.smem > sums ? f.smem : sums, s, p);
+    return (int)UNIPOOL_OK;
+  };
+  return f.cluster ? run(std::integral_constant<int, kNormBwdCluster>()) : run(std::integral_constant<int, 1>());
 }
 
 template <typename E> int norm_bwd_as(unipool_ctx* ctx, NormBwdParams p, bool aligned, float* scratch, bool overwrite, cudaStream_t s) {
   constexpr int V = 16 / (int)sizeof(E);
-  const NormBwdShape f = norm_bwd_shape(ctx, p.T, p.width, aligned, p.dr != nullptr ? 3 : 2);
+  NormBwdShape f = norm_bwd_shape(ctx, p.T, p.width, aligned, p.dr != nullptr ? 3 : 2);
   float* dw = p.dw;
-  const bool split = dw != nullptr && f.blocks > 1;
+  f.cluster = f.cluster && dw != nullptr;
+  const bool split = dw != nullptr && f.blocks > 1 && !f.cluster;
   p.add = !overwrite && !split;
   p.stages = f.stages;
   if (split) p.dw = scratch;
@@ -532,8 +560,8 @@ template <typename E> int norm_bwd_as(unipool_ctx* ctx, NormBwdParams p, bool al
 size_t rmsnorm_bwd_scratch(const unipool_ctx* ctx, int T, int width) {
   int most = 0;
   for (int k = 0; k < 4; ++k) {
-    const int n = norm_bwd_shape(ctx, T, width, (k & 1) != 0, k < 2 ? 2 : 3).blocks;
-    most = n > most ? n : most;
+    const NormBwdShape f = norm_bwd_shape(ctx, T, width, (k & 1) != 0, k < 2 ? 2 : 3);
+    if (!f.cluster && f.blocks > most) most = f.blocks;
   }
   return most > 1 ? (size_t)most * width * sizeof(float) : 0;
 }
