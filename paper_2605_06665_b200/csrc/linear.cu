@@ -332,14 +332,23 @@ template <Major BM> int rows_simt(unipool_ctx* ctx, int phase, const SimtLinear&
   return rows_as<SimtBlockTile<1>, BM, 1>(ctx, phase, p, s);
 }
 
-// Parts of the tokens for the weight gradient: two blocks of tiles to an SM, 256 tokens at least to a part.  (Tiles of 128 x 128 were no
-// faster: 16384 tokens 768 x 1024 622/622 us, 3000 of 4096 x 1536 807/770.)
+// Tokens of a part of the weight gradient: the number of parts with the least time, by the blocks on the fullest SM (a block of 64 x 64
+// takes 24 ns a token beside two others, 27 beside one and 33 alone), their starts, and writing and reading the parts' sums (8 bytes a
+// ns).  us with one part / two blocks to an SM / this: 2183 tokens 1728 x 256 78/60/49, 2000 2048 x 1024 203/203/175, 16384 768 x 1024
+// 882/622/525, 512 256 x 512 20/13/9.  (Tiles of 128 x 128 were no faster.)
 int dw_length_simt(const unipool_ctx* ctx, int T, int n_in, int n_out) {
-  const int tiles = (n_out / 64) * (n_in / 64);
-  int n = (2 * ctx->sm_count + tiles - 1) / tiles;
-  if (n > (T + 255) / 256) n = (T + 255) / 256;
-  if (n < 1) n = 1;
-  return ((T + n - 1) / n + kSimtKC - 1) / kSimtKC * kSimtKC;
+  const int64_t tiles = (int64_t)(n_out / 64) * (n_in / 64);
+  int best = 0;
+  double least = 0.0;
+  for (int n = 1; n <= 64 && n <= (T + 63) / 64; ++n) {
+    const int len = ((T + n - 1) / n + kSimtKC - 1) / kSimtKC * kSimtKC;
+    if ((T + len - 1) / len != n) continue;
+    const double k = (double)((tiles * n + ctx->sm_count - 1) / ctx->sm_count);
+    double us = k * (len * (k > 2.0 ? 0.025 : k > 1.0 ? 0.027 : 0.033) + 0.35);
+    if (n > 1) us += 2.0 + (double)n * n_in * n_out / 1.0e6;
+    if (best == 0 || us < least) { best = len; least = us; }
+  }
+  return best;
 }
 int dw_splits_simt(const unipool_ctx* ctx, int T, int n_in, int n_out) {
   const int len = dw_length_simt(ctx, T, n_in, n_out);
