@@ -405,7 +405,7 @@ int unipool_quantize_rows(unipool_ctx* ctx, const void* x, int32_t rows, int32_t
  *      (ctx dtype) or NULL.
  * out: y [T,n_out] (ctx dtype; may be residual); pre [T,n_out] (ctx dtype; p, which the backward call of an
  *      activation needs) or NULL.
- * In a bf16 context the arrays of ctx dtype are 16-byte aligned. */
+ * x is none of the outputs.  In a bf16 context the arrays of ctx dtype are 16-byte aligned. */
 int unipool_linear(unipool_ctx* ctx, const void* x, int32_t T, int32_t n_in, const void* W, int32_t n_out,
                    const float* bias, int32_t act, const void* residual, void* pre, void* y, unipool_stream stream);
 
@@ -425,8 +425,9 @@ int unipool_linear_scaled(unipool_ctx* ctx, const uint8_t* x, const float* x_sca
  *      with UNIPOOL_ACT_NONE; dp may be pre or dy); x, W of the forward call (x is needed for dW, W for dx);
  *      dx_residual [T,n_in] or NULL; scratch: unipool_linear_bwd_scratch() bytes of device memory, 16-byte aligned,
  *      which the call may use until it is complete on the stream (may be NULL where that is 0, or dW and dbias are NULL).
- * out: dx [T,n_in] (ctx dtype, overwritten; may be dx_residual) or NULL; dW [n_out,n_in] float += or NULL (16-byte
- *      aligned in a bf16 context); dbias [n_out] float += or NULL.
+ * out: dx [T,n_in] (ctx dtype, overwritten; may be dx_residual, not an operand of the products: dp, dy with
+ *      UNIPOOL_ACT_NONE, x with dW) or NULL; dW [n_out,n_in] float += or NULL (16-byte aligned in a bf16 context);
+ *      dbias [n_out] float += or NULL.
  * flags: 0 or UNIPOOL_WGRAD_OVERWRITE (dW and dbias are written, not added to). */
 int unipool_linear_bwd(unipool_ctx* ctx, const void* dy, int32_t T, int32_t n_out, const void* pre, int32_t act,
                        const void* x, int32_t n_in, const void* W, void* dp, const void* dx_residual, void* dx, float* dW,

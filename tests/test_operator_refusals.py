@@ -97,7 +97,7 @@ def test_quantize_rows(lib, ctx):
 
 
 def linear_args(ctx):
-    return dict(ctx=ctx, x=P, T=10, n_in=128, W=P, n_out=192, bias=P, act=1, residual=P, pre=2 * P, y=P, stream=None)
+    return dict(ctx=ctx, x=4 * P, T=10, n_in=128, W=P, n_out=192, bias=P, act=1, residual=P, pre=2 * P, y=P, stream=None)
 
 
 def check_features(f):
@@ -113,7 +113,7 @@ def test_linear(lib, ctx):
         assert f(**c) == 0, c
     for n in ("ctx", "x", "W", "y"):
         assert f(**{n: None}) == ARG, n
-    for c in (dict(act=-1), dict(act=4), dict(T=-1), dict(T=101), dict(pre=P)):
+    for c in (dict(act=-1), dict(act=4), dict(T=-1), dict(T=101), dict(pre=P), dict(x=P), dict(x=2 * P)):   # (x is y, x is pre)
         assert f(**c) == ARG, c
     check_features(f)
     for n in ("x", "W", "residual", "pre", "y"):             # moved by TMA on the tensor-core path
@@ -122,7 +122,7 @@ def test_linear(lib, ctx):
 
 def test_linear_scaled(lib, ctx):
     a = linear_args(ctx)
-    a = dict(ctx=ctx, x=P, x_scale=P, T=10, n_in=128, W=P, w_scale=P, **{n: a[n] for n in ("n_out", "bias", "act", "residual", "pre", "y", "stream")})
+    a = dict(ctx=ctx, x=4 * P, x_scale=P, T=10, n_in=128, W=P, w_scale=P, **{n: a[n] for n in ("n_out", "bias", "act", "residual", "pre", "y", "stream")})
     f = lambda **c: call(lib, "linear_scaled", a, **c)
     if not ctx.bf16:
         assert f() == UNSUPPORTED
@@ -136,15 +136,18 @@ def test_linear_scaled(lib, ctx):
 
 
 def test_linear_backward(lib, ctx):
-    a = dict(ctx=ctx, dy=P, T=10, n_out=192, pre=P, act=2, x=P, n_in=128, W=P, dp=P, dx_residual=P, dx=P, dW=P, dbias=P,
+    a = dict(ctx=ctx, dy=P, T=10, n_out=192, pre=P, act=2, x=P, n_in=128, W=P, dp=P, dx_residual=P, dx=3 * P, dW=P, dbias=P,
              scratch=P, flags=0, stream=None)
     f = lambda **c: call(lib, "linear_bwd", a, **c)
     for c in ({}, dict(act=0, pre=None, dp=None), dict(dW=None, dbias=None, scratch=None, x=None), dict(dx=None, W=None),
               dict(flags=B.WGRAD_OVERWRITE), dict(T=0, scratch=None), dict(dx_residual=None)):
         assert f(**c) == 0, c
     for c in (dict(ctx=None), dict(dy=None), dict(pre=None), dict(dp=None), dict(x=None), dict(W=None), dict(act=4), dict(T=101),
-              dict(dx=None, dW=None, dbias=None), dict(flags=1), dict(flags=8)):
+              dict(dx=None, dW=None, dbias=None), dict(flags=1), dict(flags=8), dict(dx=P), dict(dx=P, x=2 * P), dict(dx=P, dp=2 * P),
+              dict(dx=P, x=2 * P, act=0)):
         assert f(**c) == ARG, c
+    for c in (dict(dx=P, x=2 * P, dp=2 * P), dict(dx=P, dp=2 * P, dW=None)):   # onto dy or x that no product reads
+        assert f(**c) == 0, c
     check_features(f)
     assert f(scratch=None) == WORKSPACE and f(scratch=P + 8) == WORKSPACE
     for n in ("dy", "pre", "dp", "x", "W", "dx_residual", "dx", "dW"):
