@@ -469,7 +469,7 @@ static int linear_call(unipool_ctx* ctx, const LinearArgs& a, unipool_stream str
   CHECK_T(ctx, a.T); CHECK_FEATURES(n_in); CHECK_FEATURES(n_out); CHECK_ACT(a.act);
   CHECK_PTR(x); CHECK_PTR(W); CHECK_PTR(y);
   UP_REQUIRE(pre == nullptr || (pre != y && pre != residual), UNIPOOL_ERR_INVALID_ARG, "pre is y or residual");
-  UP_REQUIRE(y != x && pre != x, UNIPOOL_ERR_INVALID_ARG, "x, which other tiles still read, is y or pre");
+  UP_REQUIRE(a.T == 0 || (y != x && pre != x), UNIPOOL_ERR_INVALID_ARG, "x, which other tiles still read, is y or pre");
   CHECK_ALIGNED(ctx, x); CHECK_ALIGNED(ctx, W); CHECK_ALIGNED(ctx, residual); CHECK_ALIGNED(ctx, pre); CHECK_ALIGNED(ctx, y);
   return linear_launch(ctx, a, static_cast<cudaStream_t>(stream));
 }
@@ -504,7 +504,7 @@ int unipool_linear_bwd(unipool_ctx* ctx, const void* dy, int32_t T, int32_t n_ou
   UP_REQUIRE((flags & ~UNIPOOL_WGRAD_OVERWRITE) == 0, UNIPOOL_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
   if (dx != nullptr) CHECK_PTR(W);
   if (dW != nullptr) CHECK_PTR(x);
-  UP_REQUIRE(dx == nullptr || (dx != (act != UNIPOOL_ACT_NONE ? dp : dy) && (dW == nullptr || dx != x)), UNIPOOL_ERR_INVALID_ARG,
+  UP_REQUIRE(T == 0 || dx == nullptr || (dx != (act != UNIPOOL_ACT_NONE ? dp : dy) && (dW == nullptr || dx != x)), UNIPOOL_ERR_INVALID_ARG,
              "dx is an operand of the products: dp (dy without an activation), or x");
   // (its size, which takes a search, only where it decides)
   if ((dW != nullptr || dbias != nullptr) && T > 0 && (scratch == nullptr || (reinterpret_cast<uintptr_t>(scratch) & 15) != 0) &&

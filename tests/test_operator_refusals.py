@@ -109,7 +109,7 @@ def check_features(f):
 def test_linear(lib, ctx):
     a = linear_args(ctx)
     f = lambda **c: call(lib, "linear", a, **c)
-    for c in ({}, dict(bias=None, residual=None, pre=None, act=0), dict(T=0), dict(T=100), dict(act=3), dict(bias=P + 4), dict(residual=P, y=P)):
+    for c in ({}, dict(bias=None, residual=None, pre=None, act=0), dict(T=0), dict(T=100), dict(act=3), dict(bias=P + 4), dict(residual=P, y=P), dict(T=0, x=P)):
         assert f(**c) == 0, c
     for n in ("ctx", "x", "W", "y"):
         assert f(**{n: None}) == ARG, n
