@@ -376,7 +376,8 @@ int unipool_rmsnorm(unipool_ctx* ctx, const void* x, const void* y, int32_t T, i
  * (dx is the gradient of x and of y alike; dr that of r itself, which the residual stream brings).
  * in : dh [T,width]; r [T,width] as the forward call stored it (its x where it had no y); w; rstd; dr [T,width] or
  *      NULL; scratch: unipool_rmsnorm_bwd_scratch() bytes of device memory, 16-byte aligned, which the call may
- *      use until it is complete on the stream (may be NULL where that is 0 or dw is NULL).
+ *      use until it is complete on the stream (may be NULL where that is 0 or dw is NULL); what some rows need is
+ *      enough for fewer rows of that width.
  * out: dx [T,width] (ctx dtype, overwritten; may be dh, r or dr); dw [width] float +=, or NULL.
  * flags: 0 or UNIPOOL_WGRAD_OVERWRITE (dw is written, not added to).  The sums over the rows are taken in an order
  * that depends on T and width alone. */
@@ -424,7 +425,8 @@ int unipool_linear_scaled(unipool_ctx* ctx, const uint8_t* x, const float* x_sca
  * in : dy [T,n_out]; pre [T,n_out] of the forward call and dp [T,n_out], scratch that is overwritten (both NULL
  *      with UNIPOOL_ACT_NONE; dp may be pre or dy); x, W of the forward call (x is needed for dW, W for dx);
  *      dx_residual [T,n_in] or NULL; scratch: unipool_linear_bwd_scratch() bytes of device memory, 16-byte aligned,
- *      which the call may use until it is complete on the stream (may be NULL where that is 0, or dW and dbias are NULL).
+ *      which the call may use until it is complete on the stream (may be NULL where that is 0, or dW and dbias are NULL):
+ *      for these T, n_in and n_out, since fewer tokens may be cut into more parts.
  * out: dx [T,n_in] (ctx dtype, overwritten; may be dx_residual, not an operand of the products: dp, dy with
  *      UNIPOOL_ACT_NONE, x with dW) or NULL; dW [n_out,n_in] float += or NULL (16-byte aligned in a bf16 context);
  *      dbias [n_out] float += or NULL.

@@ -264,6 +264,13 @@ def test_scratch_of_the_callers(mode):
         ctx.rmsnorm_bwd(dh, r, T, width, w, rstd, None, dx, got, scratch=whole[:n - 1])
 
 
+def test_scratch_of_many_rows_is_enough_for_fewer(mode):
+    ctx, _ = mode
+    for width in (1, 64, 768, 1001, 1536, 4096, 9473, 16384):
+        sizes = [ctx.rmsnorm_bwd_scratch(T, width) for T in (*range(1, 300), 500, 1000, 3000, 8192)]
+        assert sizes == sorted(sizes), width
+
+
 def test_no_rows(mode):
     ctx, dt = mode
     from paper_2605_06665_b200 import binding as B
