@@ -8,7 +8,8 @@
 // Bound by HBM: forward 2 (x, h) to 4 (y, r too) passes over the stream, backward 3 to 4, next to no arithmetic.  A row stays
 // in the registers of the threads that share it, so that it is read once: a warp up to 256 vectors of 16 bytes (2048 bf16
 // columns), four or sixteen warps beyond; all of a thread's loads are issued before the first is used.  Rows whose bytes are no
-// multiple of 16, and misaligned tensors, go element by element through the same kernels.
+// multiple of 16, and misaligned tensors, go two elements or one at a time through the same kernels.  16384 x 768 bf16 with residual 17 us
+// (5.9 TB/s), 32768 x 1536 with 8 bits too 71 us (6.4 TB/s); backward of 16384 x 768 with dr 22 us, 4 of them for adding up dw.
 // Sums of squares, the statistics and the gradient of w are fp32; h is formed from the unrounded sum r.
 #include <cooperative_groups.h>
 #include <cuda_fp8.h>
@@ -501,11 +502,16 @@ template <bool kNorm, typename E> int norm_as(unipool_ctx* ctx, const NormParams
   }
   auto narrow = [&](auto v) {
     const int n = p.width / decltype(v)::value;
+    // Sixteen vectors to a thread leave fewer rows in work at a time, with more bytes under way for each: better for many rows (us, eight and
+    // sixteen vectors: 16384 x 301 bf16 16.2 and 10.4, 24702 x 2187 100 and 86, 4096 x 3001 24 and 22), worse for few (1 x 1001 2.9
+    // and 4.3) and for rows of 513 to 2048 (16384 x 1001 fp32 42 and 50).
+    const bool many = p.T > 8 * ctx->sm_count;
     if (n <= 256) return run(v, Int<32>(), Int<8>());
+    if (n <= 512 && many) return run(v, Int<32>(), Int<16>());
     if (n <= 1024) return run(v, Int<128>(), Int<8>());
     if (n <= 2048) return run(v, Int<256>(), Int<8>());
-    if (n <= 2560) return run(v, Int<320>(), Int<8>());
-    if (n <= 4096) return run(v, Int<512>(), Int<8>());
+    if (n <= 2560) return many ? run(v, Int<160>(), Int<16>()) : run(v, Int<320>(), Int<8>());
+    if (n <= 4096) return many ? run(v, Int<256>(), Int<16>()) : run(v, Int<512>(), Int<8>());
     return run(v, Int<512>(), Int<32>());
   };
   return fits(2) ? narrow(Int<2>()) : narrow(Int<1>());

@@ -95,6 +95,11 @@ def test_forward(mode, T, width, with_y):
     assert torch.equal(h2, h) and torch.equal(q2.view(torch.uint8), q.view(torch.uint8)) and torch.equal(scale2, scale)
 
 
+@pytest.mark.parametrize("width", [301, 770, 1001, 2187, 4374, 3001, 6002])
+def test_forward_of_many_rows_of_any_width(mode, width):
+    test_forward(mode, 1301, width, True)
+
+
 @pytest.mark.parametrize("T,width", SIZES)
 @pytest.mark.parametrize("with_dr", [False, True])
 def test_backward(mode, T, width, with_dr):
