@@ -20,7 +20,7 @@ def mode(request):
     from paper_2605_06665_b200 import build as builder
     builder.build()
     code, dt = (B.BF16, torch.bfloat16) if request.param == "bf16" else (B.FP32, torch.float32)
-    ctx = B.Context(B.make_config(64, 64, 1, 1, 1, 4096, code, EPS, 1.0))
+    ctx = B.Context(B.make_config(64, 64, 1, 1, 1, 8192, code, EPS, 1.0))
     yield ctx, dt
     ctx.check_status()
     ctx.close()
@@ -129,6 +129,11 @@ def test_backward(mode, T, width, with_dr):
     assert torch.equal(dw2, dw + 3.0) and torch.equal(dx2, dx)
     ctx.rmsnorm_bwd(dh, r, T, width, w, rstd, dr, dx2.zero_(), None)
     assert torch.equal(dx2, dx)
+
+
+@pytest.mark.parametrize("width", [301, 770, 1001, 1538])
+def test_backward_of_many_rows_of_any_width(mode, width):
+    test_backward(mode, 5003, width, True)
 
 
 def test_gradient_by_differences(mode):
