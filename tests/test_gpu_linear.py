@@ -424,10 +424,11 @@ def test_misaligned_fp32():
         m.ctx.close()
 
 
-def test_captured_calls_on_two_streams(train):
+@pytest.mark.parametrize("T", [40, 200, 900])
+def test_captured_calls_on_two_streams(train, T):
     """Forward and backward recorded twice, each with scratch of its own, replayed on two streams at once."""
     m = train
-    T, n_in, n_out, act = 900, 256, 384, "silu"
+    n_in, n_out, act = 256, 384, "silu"
     sets = []
     for i in range(2):
         d = backward_case(m, T, n_in, n_out, act, seed=50 + 10 * i)
