@@ -2,7 +2,8 @@
 //   forward   y  = act(x W^T s_x s_w + bias) + residual   x, W K-major, bf16 or e4m3 with scales
 //   dx        dx = dp W (+ dx_residual)                   W MN-major
 //   dW        dW (+)= dp^T x                              both MN-major, fp32 out
-// Three forms: CTA pairs with tiles of 256 x 256 or 256 x 128, and a kernel for few tokens (below); the rule is linear_form.
+// Three forms: CTA pairs with tiles of 256 x 256 or 256 x 128, and a kernel for few tokens (below); the rule is linear_form.  dx and dW may
+// share a launch of CTA pairs (linear_dw_plan_tc).
 //
 // linear_pair_kernel: persistent CTA pairs as in the grouped kernels (expert_tc.cu): 256 x 256 tiles, M = 256 over both CTAs'
 // tensor memory, six 32 KB operand stages a CTA, accumulators double-buffered so that a tile's epilogue runs beside the next
@@ -10,7 +11,9 @@
 // waits (tensor memory, shared memory, proxy fence, TMA) of a microsecond, which it takes four warps on a scheduler to hide behind
 // the products of 768 inputs, the special-function unit (two instructions an element of silu and gelu) being busy for 2.2 of
 // the 3.1 us that they take.
-// Bound by the tensor pipe (operands through shared memory; see expert_tc.cu) and, held for long, by power.
+// Bound by the tensor pipe (operands through shared memory; see expert_tc.cu) and, held for long, by power: 9001 tokens 1536 -> 4096 79 us
+// (1.44 PFLOP/s), in e4m3 50 us (2.28 PFLOP/s), 16384 tokens 768 -> 2048 42 us, with gelu 46, with p stored too 52.  With few tiles of a long
+// contraction by what the L2 delivers (1501 tokens 4096 -> 1536: 72 tiles of 256 x 128, 26 us).
 #include <cuda.h>
 
 #include <algorithm>
@@ -824,25 +827,29 @@ int linear_dx_tc(unipool_ctx* ctx, const LinearBwdArgs& a, const void* dp, cudaS
 }
 
 // How the weight gradient is taken: the parts of the tokens, so that its tiles fill the CTA pairs, and whether dx's tiles go into the same
-// launch behind its own (short tiles after long ones).  Each by its time in us: rounds of tiles (0.3 us a k-block), the parts' sums
-// (6 bytes a ns written and read, and a launch), a launch between two kernels.
+// launch behind its own (short tiles after long ones).  Each by its time in us: a pair's tiles (0.29 us a k-block, 0.38 while all pairs are
+// busy, an epilogue at least), the parts' sums (6 bytes a ns written and read, and a launch), a launch between two kernels.  Measured
+// in us (tokens, n_in, n_out), two launches / one with 128 columns / with 256:
+//   8 192 3584 13/21/22      128 2048 768 18/9/11     493 1408 960 20/11/12     820 4096 1536 32/36/27   1501 768 2048 28/24/17
+//   1501 1536 4096 49/50/36  4000 256 512 20/12/14    4000 1536 4096 96/128/78  16384 768 2048 88/127/88  32768 1536 1536 239/338/239
 LinearDwPlan linear_dw_plan_tc(const unipool_ctx* ctx, int T, int n_in, int n_out, bool with_dx) {
   const int kb = (T + 63) / 64, pairs = ctx->sm_count / 2, kb_x = n_out / 64;
   LinearDwPlan best{1, 0};
   double least = 0.0;
   const double apart = with_dx ? linear_form(ctx, T, n_in, kb_x, true).us + kLaunchUs + 3.3 : 0.0;
   auto consider = [&](int tile, bool together) {
-    const int tiles = ((n_out + 255) / 256) * ((n_in + tile - 1) / tile), units_x = together ? ((T + 255) / 256) * ((n_in + tile - 1) / tile) : 0;
+    const int across = (n_in + tile - 1) / tile, tiles = ((n_out + 255) / 256) * across;
+    const int64_t units_x = together ? ((int64_t)T + 255) / 256 * across : 0;
     const double end = tile == 256 ? 3.5 : 2.0;
     for (int splits = 1; splits <= 64 && splits <= kb && (splits == 1 || tiles * (splits - 1) < 2 * pairs); ++splits) {
       const int len = (kb + splits - 1) / splits, parts = (kb + len - 1) / len;
       if (parts != splits) continue;
       // pair q takes units q, q + pairs, ...; the last to end is the first of one of these
-      const int units_w = tiles * splits, all = units_w + units_x;
+      const int64_t units_w = (int64_t)tiles * splits, all = units_w + units_x;
       double us = 0.0;
-      for (const int q : {0, units_w % pairs, all % pairs}) {
-        const int n = (all - q + pairs - 1) / pairs, w = q < units_w ? (units_w - q + pairs - 1) / pairs : 0;
-        const double busy = ((double)units_w * len + (double)units_x * kb_x) / ((double)pairs * (w * len + (n - w) * kb_x));
+      for (const int64_t q : {(int64_t)0, units_w % pairs, all % pairs}) {
+        const int64_t n = (all - q + pairs - 1) / pairs, w = q < units_w ? (units_w - q + pairs - 1) / pairs : 0;
+        const double busy = ((double)units_w * len + (double)units_x * kb_x) / ((double)pairs * (double)(w * len + (n - w) * kb_x));
         const double each = 0.29 + 0.09 * std::min(1.0, busy * busy);
         us = std::max(us, w * std::max(len * each + 1.0, end) + (n - w) * std::max(kb_x * each + 1.0, end));
       }
