@@ -474,8 +474,15 @@ template <typename... P> bool aligned(uintptr_t n, P... p) { return ((... | rein
 // share a tile's contraction and add up through each other's shared memory, in the order of their ranks; each then finishes every
 // S-th token.  Bound by the weights' bytes and, below some megabytes of them, by latency: every CTA asks for all of its weights
 // at once as far as they fit its stages.
+// No CTA waits for another one while it holds tensor memory: the columns go back as soon as the sums lie in shared memory, in front of the
+// first wait for the cluster.  (CTAs of several calls share an SM where those run on several streams, and an allocation waits until
+// columns are free: one that is held until the cluster is complete could wait for a CTA that itself waits for columns, round in a ring.)
+// And every launch asks for so much shared memory that no more CTAs lie on an SM than it has columns for.
 constexpr int kFewTokens = 128, kFewMaxStages = 12;
 constexpr uint32_t kFewBars = 512;
+constexpr uint32_t kFewColumns = 128;                    // of the SM's 512: one accumulator of up to 128 tokens
+constexpr uint32_t kFewSmemLeast = 46080;                // (with the system's 1 KB, five CTAs are more than an SM's 228 KB)
+static_assert(kFewColumns >= kFewTokens && (512 / kFewColumns + 1) * (kFewSmemLeast + 1024) > 228 * 1024, "tensor memory of an SM");
 
 struct FewParams {
   int T, M, N;                       // tokens of the call and of a tile (a multiple of 16); features of the result
@@ -528,7 +535,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     tc::tma_prefetch_desc(&tmX);
   }
   if (warp == 1) {
-    tc::tmem_alloc(tmem_ptr, 128);
+    tc::tmem_alloc(tmem_ptr, kFewColumns);
     tc::tmem_relinquish();
   }
   tc::tc_fence_before_sync();
@@ -601,7 +608,12 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
     }
     tc::tc_fence_before_sync();
   }
-  if constexpr (S > 1) tc::cluster_sync(); else __syncthreads();   // every CTA's sums are there
+  __syncthreads();                                       // this CTA's sums are there
+  if (warp == 1) {
+    tc::tc_fence_after_sync();
+    tc::tmem_dealloc(tmem, kFewColumns);                  // (before any other CTA is waited for)
+  }
+  if constexpr (S > 1) tc::cluster_sync();               // every CTA's are
 
   // Four features to a lane, a token to a warp: of the cluster's (2 + E) S warps each takes every (2 + E) S-th token.
   const int m = m0 + 4 * lane;
@@ -639,11 +651,7 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
       store_bf16x4(&p.y[at], v);
     }
   }
-  if constexpr (S > 1) tc::cluster_sync(); else __syncthreads();   // no CTA leaves while another reads its sums
-  if (warp == 1) {
-    tc::tc_fence_after_sync();
-    tc::tmem_dealloc(tmem, 128);
-  }
+  if constexpr (S > 1) tc::cluster_sync();               // no CTA leaves while another reads its sums
 }
 
 template <int KIND, int S, int E>
@@ -712,7 +720,7 @@ int few_as(unipool_ctx* ctx, int phase, const CUtensorMap& tmW, const CUtensorMa
   auto as = [&](auto e) {
     constexpr int E = decltype(e)::value;
     auto run = splits == 8 ? launch_few<KIND, 8, E> : splits == 4 ? launch_few<KIND, 4, E> : splits == 2 ? launch_few<KIND, 2, E> : launch_few<KIND, 1, E>;
-    return run(ctx, phase, tmW, tmX, p, 2048 + bytes, s);
+    return run(ctx, phase, tmW, tmX, p, std::max(2048 + bytes, kFewSmemLeast), s);
   };
   return f.wide ? as(std::integral_constant<int, 16>()) : as(std::integral_constant<int, 4>());
 }
