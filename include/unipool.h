@@ -23,6 +23,8 @@
  *   - Calls are asynchronous on `stream` and never synchronise the host: group
  *     sizes stay on the device.  Calls of one context must be issued on one
  *     stream at a time (they share the workspace).
+ *   - unipool_rmsnorm, unipool_linear and the calls beside them take no tokens too: T (or rows) = 0 leaves every array of
+ *     that dimension alone, and those may be NULL.
  *   - Arguments marked "+=" accumulate into what the buffer holds.
  *
  * Permuted ("expert-contiguous") row space

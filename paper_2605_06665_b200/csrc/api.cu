@@ -416,14 +416,17 @@ int unipool_route_bwd(unipool_ctx* ctx, const void* x, int32_t T, const float* W
                           dscore_coef, dx, dW_r, dsigma, static_cast<cudaStream_t>(stream));
 }
 
+// (Arrays of no tokens have no address: the operators below require those of a dimension T, or rows, only where it is not 0.)
 #define CHECK_WIDTH(n)                                                                           \
   UP_REQUIRE((n) >= 1 && (n) <= kNormMaxWidth, UNIPOOL_ERR_UNSUPPORTED, "width = %d outside [1, %d]", (int)(n), kNormMaxWidth)
 
 int unipool_rmsnorm(unipool_ctx* ctx, const void* x, const void* y, int32_t T, int32_t width, const float* w, float eps,
                     void* r, float* rstd, void* h, uint8_t* q, float* q_scale, unipool_stream stream) {
   CHECK_CTX(ctx); CHECK_DEVICE(ctx); CHECK_T(ctx, T); CHECK_WIDTH(width);
-  CHECK_PTR(x); CHECK_PTR(w);
+  CHECK_PTR(w);
   UP_REQUIRE(eps >= 0.f, UNIPOOL_ERR_INVALID_ARG, "eps must be >= 0");
+  if (T == 0) return UNIPOOL_OK;
+  CHECK_PTR(x);
   UP_REQUIRE(h != nullptr || q != nullptr, UNIPOOL_ERR_INVALID_ARG, "h and q are both NULL");
   UP_REQUIRE((q != nullptr) == (q_scale != nullptr), UNIPOOL_ERR_INVALID_ARG, "q and q_scale go together");
   UP_REQUIRE(r == nullptr || r != h, UNIPOOL_ERR_INVALID_ARG, "r and h are the same array");
@@ -438,7 +441,8 @@ int unipool_rmsnorm_bwd(unipool_ctx* ctx, const void* dh, const void* r, int32_t
                         const float* rstd, const void* dr, void* dx, float* dw, void* scratch, int32_t flags,
                         unipool_stream stream) {
   CHECK_CTX(ctx); CHECK_DEVICE(ctx); CHECK_T(ctx, T); CHECK_WIDTH(width);
-  CHECK_PTR(dh); CHECK_PTR(r); CHECK_PTR(w); CHECK_PTR(rstd); CHECK_PTR(dx);
+  CHECK_PTR(w);
+  if (T > 0) { CHECK_PTR(dh); CHECK_PTR(r); CHECK_PTR(rstd); CHECK_PTR(dx); }
   UP_REQUIRE((flags & ~UNIPOOL_WGRAD_OVERWRITE) == 0, UNIPOOL_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
   if (dw != nullptr && T > 0 && rmsnorm_bwd_scratch(ctx, T, width) > 0) CHECK_SCRATCH(scratch);
   return rmsnorm_bwd_launch(ctx, dh, r, T, width, w, rstd, dr, dx, dw, static_cast<float*>(scratch),
@@ -449,7 +453,7 @@ int unipool_quantize_rows(unipool_ctx* ctx, const void* x, int32_t rows, int32_t
                           unipool_stream stream) {
   CHECK_CTX(ctx); CHECK_DEVICE(ctx); CHECK_WIDTH(width);
   UP_REQUIRE(rows >= 0, UNIPOOL_ERR_INVALID_ARG, "rows = %d is negative", rows);
-  CHECK_PTR(x); CHECK_PTR(q); CHECK_PTR(q_scale);
+  if (rows > 0) { CHECK_PTR(x); CHECK_PTR(q); CHECK_PTR(q_scale); }
   return quantize_rows_launch(ctx, x, rows, width, q, q_scale, static_cast<cudaStream_t>(stream));
 }
 
@@ -467,7 +471,8 @@ static int linear_call(unipool_ctx* ctx, const LinearArgs& a, unipool_stream str
   const void *x = a.x, *W = a.W, *residual = a.residual, *pre = a.pre, *y = a.y;
   const int n_in = a.n_in, n_out = a.n_out;
   CHECK_T(ctx, a.T); CHECK_FEATURES(n_in); CHECK_FEATURES(n_out); CHECK_ACT(a.act);
-  CHECK_PTR(x); CHECK_PTR(W); CHECK_PTR(y);
+  CHECK_PTR(W);
+  if (a.T > 0) { CHECK_PTR(x); CHECK_PTR(y); }
   UP_REQUIRE(pre == nullptr || (pre != y && pre != residual), UNIPOOL_ERR_INVALID_ARG, "pre is y or residual");
   UP_REQUIRE(a.T == 0 || (y != x && pre != x), UNIPOOL_ERR_INVALID_ARG, "x, which other tiles still read, is y or pre");
   CHECK_ALIGNED(ctx, x); CHECK_ALIGNED(ctx, W); CHECK_ALIGNED(ctx, residual); CHECK_ALIGNED(ctx, pre); CHECK_ALIGNED(ctx, y);
@@ -483,7 +488,8 @@ int unipool_linear(unipool_ctx* ctx, const void* x, int32_t T, int32_t n_in, con
 int unipool_linear_scaled(unipool_ctx* ctx, const uint8_t* x, const float* x_scale, int32_t T, int32_t n_in,
                           const uint8_t* W, const float* w_scale, int32_t n_out, const float* bias, int32_t act,
                           const void* residual, void* pre, void* y, unipool_stream stream) {
-  CHECK_CTX(ctx); CHECK_DEVICE(ctx); CHECK_PTR(x_scale); CHECK_PTR(w_scale);
+  CHECK_CTX(ctx); CHECK_DEVICE(ctx); CHECK_PTR(w_scale);
+  if (T != 0) CHECK_PTR(x_scale);
   UP_REQUIRE(use_tensor_cores(ctx), UNIPOOL_ERR_UNSUPPORTED, "8-bit operands need a bf16 context");
   return linear_call(ctx, LinearArgs{x, W, x_scale, w_scale, T, n_in, n_out, act, bias, residual, pre, y}, stream);
 }
@@ -498,12 +504,14 @@ int unipool_linear_bwd(unipool_ctx* ctx, const void* dy, int32_t T, int32_t n_ou
                        const void* x, int32_t n_in, const void* W, void* dp, const void* dx_residual, void* dx, float* dW,
                        float* dbias, void* scratch, int32_t flags, unipool_stream stream) {
   CHECK_CTX(ctx); CHECK_DEVICE(ctx); CHECK_T(ctx, T); CHECK_FEATURES(n_in); CHECK_FEATURES(n_out); CHECK_ACT(act);
-  CHECK_PTR(dy);
-  if (act != UNIPOOL_ACT_NONE) { CHECK_PTR(pre); CHECK_PTR(dp); }
-  UP_REQUIRE(dx != nullptr || dW != nullptr || dbias != nullptr, UNIPOOL_ERR_INVALID_ARG, "dx, dW and dbias are all NULL");
+  if (T > 0) {
+    CHECK_PTR(dy);
+    if (act != UNIPOOL_ACT_NONE) { CHECK_PTR(pre); CHECK_PTR(dp); }
+    UP_REQUIRE(dx != nullptr || dW != nullptr || dbias != nullptr, UNIPOOL_ERR_INVALID_ARG, "dx, dW and dbias are all NULL");
+    if (dW != nullptr) CHECK_PTR(x);
+  }
   UP_REQUIRE((flags & ~UNIPOOL_WGRAD_OVERWRITE) == 0, UNIPOOL_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
   if (dx != nullptr) CHECK_PTR(W);
-  if (dW != nullptr) CHECK_PTR(x);
   UP_REQUIRE(T == 0 || dx == nullptr || (dx != (act != UNIPOOL_ACT_NONE ? dp : dy) && (dW == nullptr || dx != x)), UNIPOOL_ERR_INVALID_ARG,
              "dx is an operand of the products: dp (dy without an activation), or x");
   // (its size, which takes a search, only where it decides)

@@ -184,3 +184,25 @@ def test_binding_takes_dense_tensors_only():
     for t in (a.t(), a[:, :3], a[::2], a[0].expand(4, 6)):
         with pytest.raises(ValueError):
             B._d(t)
+
+
+def test_no_tokens_need_no_arrays_of_tokens(lib, ctx):
+    """What an empty batch hands over: x[:0] has no address.  Weights are checked as ever."""
+    norm = dict(norm_args(ctx), T=0, x=None, y=None, r=None, rstd=None, h=None)
+    back = dict(ctx=ctx, dh=None, r=None, T=0, width=768, w=P, rstd=None, dr=None, dx=None, dw=P, scratch=None, flags=0, stream=None)
+    rows = dict(ctx=ctx, x=None, rows=0, width=96, q=None, q_scale=None, stream=None)
+    linear = dict(linear_args(ctx), T=0, x=None, residual=None, pre=None, y=None)
+    scaled = dict(ctx=ctx, x=None, x_scale=None, T=0, n_in=128, W=P, w_scale=P, n_out=192, bias=P, act=1, residual=None, pre=None, y=None, stream=None)
+    grad = dict(ctx=ctx, dy=None, T=0, n_out=192, pre=None, act=2, x=None, n_in=128, W=P, dp=None, dx_residual=None, dx=None, dW=P, dbias=P,
+                scratch=None, flags=B.WGRAD_OVERWRITE, stream=None)
+    frozen = dict(grad, dW=None, dbias=None)
+    for name, args in (("rmsnorm", norm), ("rmsnorm_bwd", back), ("quantize_rows", rows), ("linear", linear), ("linear_bwd", grad),
+                       ("linear_bwd", frozen)) + ((("linear_scaled", scaled),) if ctx.bf16 else ()):
+        assert call(lib, name, args) == 0, name
+    for name, args, weight in (("rmsnorm", norm, "w"), ("rmsnorm_bwd", back, "w"), ("linear", linear, "W")):
+        assert call(lib, name, args, **{weight: None}) == ARG, name
+    if ctx.bf16:
+        assert call(lib, "linear_scaled", scaled, w_scale=None) == ARG and call(lib, "linear_scaled", scaled, T=-1) == ARG
+    for name, args in (("rmsnorm", norm), ("rmsnorm_bwd", back), ("linear", linear), ("linear_bwd", grad)):
+        assert call(lib, name, args, T=1) == ARG and call(lib, name, args, T=-1) == ARG, name
+    assert call(lib, "quantize_rows", rows, rows=1) == ARG
