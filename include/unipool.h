@@ -413,8 +413,9 @@ int unipool_linear(unipool_ctx* ctx, const void* x, int32_t T, int32_t n_in, con
                    const float* bias, int32_t act, const void* residual, void* pre, void* y, unipool_stream stream);
 
 /* The same of operands in e4m3 with a scale for each token and each output feature (unipool_rmsnorm,
- * unipool_quantize_rows), in a bf16 context: p = x_scale[t] w_scale[o] sum_i x_ti W_oi + bias_o.  Both operands are
- * 16-byte aligned. */
+ * unipool_quantize_rows), in a bf16 context: p = ((sum_i x_ti W_oi) x_scale[t]) w_scale[o] + bias_o, the
+ * factors one after the other (the scales' own product may leave fp32's range where p does not).  Both operands
+ * are 16-byte aligned. */
 int unipool_linear_scaled(unipool_ctx* ctx, const uint8_t* x, const float* x_scale, int32_t T, int32_t n_in,
                           const uint8_t* W, const float* w_scale, int32_t n_out, const float* bias, int32_t act,
                           const void* residual, void* pre, void* y, unipool_stream stream);

@@ -369,7 +369,7 @@ linear_pair_kernel(const __grid_constant__ LinearMaps m, LinearParams p) {
           if constexpr (KIND == kLinFwd8) {
             if (kRes) c.load(p.w_scale + col, p.vec);
 #pragma unroll
-            for (int i = 0; i < 32; ++i) v[i] *= xs * c.at(i);
+            for (int i = 0; i < 32; ++i) v[i] = v[i] * xs * c.at(i);   // one after the other: their product may leave fp32's range
           }
           if ((KIND == kLinFwd8 || (KIND == kLinFwd && kRes)) && p.bias != nullptr) c.load(p.bias + col, p.vec);
           if (KIND != kLinDx && !kBoth && p.bias != nullptr) {
@@ -639,7 +639,9 @@ linear_few_kernel(const __grid_constant__ CUtensorMap tmW, const __grid_constant
         part[0].x += part[q].x; part[0].y += part[q].y; part[0].z += part[q].z; part[0].w += part[q].w;
       }
       float v[4] = {part[0].x, part[0].y, part[0].z, part[0].w};
-      if constexpr (KIND == kLinFwd8) { v[0] *= xs * ws.x; v[1] *= xs * ws.y; v[2] *= xs * ws.z; v[3] *= xs * ws.w; }
+      if constexpr (KIND == kLinFwd8) {
+        v[0] = v[0] * xs * ws.x; v[1] = v[1] * xs * ws.y; v[2] = v[2] * xs * ws.z; v[3] = v[3] * xs * ws.w;
+      }
       if constexpr (KIND != kLinDx) {
         v[0] += b.x; v[1] += b.y; v[2] += b.z; v[3] += b.w;
         if (p.pre != nullptr) store_bf16x4(&p.pre[at], v);
