@@ -140,7 +140,7 @@ __global__ void __launch_bounds__(kNormThreads<TPR>) rmsnorm_kernel(NormParams p
       float w[V];
       load_w<V>(p.w + c, w);
 #pragma unroll
-      for (int j = 0; j < V; ++j) v[i][j] *= n * w[j];
+      for (int j = 0; j < V; ++j) v[i][j] = v[i][j] * n * w[j];      // (n w may leave fp32's range where h does not)
       if (p.h != nullptr) Vec<E, V>::store(static_cast<E*>(p.h) + at + c, v[i]);
     }
   }

@@ -362,3 +362,18 @@ def test_more_than_32_bits_of_elements():
     assert ((dw - dw1).abs() <= 16 * 2.0 ** -24 * (x[rows].double() ** 2 * rs[:, None]).sum(0)).all()     # seven terms, in another order
     ctx.check_status()
     ctx.close()
+
+
+@pytest.mark.parametrize("size,weight", [(2.0 ** -60, 2.0 ** 90), (2.0 ** 40, 2.0 ** -112)])
+@pytest.mark.parametrize("width", [768, 33, 2056])
+def test_weights_at_the_ends_of_the_range(mode, size, weight, width):
+    """1 / |r| and w multiply to more than fp32 holds, or to less than its normal numbers, and h does not."""
+    ctx, dt = mode
+    T = 9
+    x = (normal((T, width), torch.float32, 60) * size).to(dt)
+    w = (1 + normal((width,), torch.float32, 61, 0.1)) * weight
+    h, q, scale = torch.empty_like(x), torch.empty(T, width, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(T, device="cuda")
+    ctx.rmsnorm(x, None, T, width, w, 0.0, None, None, h, q, scale)
+    _, _, hh = reference(x, None, w, 0.0)
+    assert ((h.double() - hh).abs() <= (half_step(dt) + FP32) * hh.abs() + 2.0 ** -133).all()      # (2^-133: bf16's smallest step)
+    check_q(q, scale, hh)
