@@ -426,8 +426,9 @@ int unipool_linear_scaled(unipool_ctx* ctx, const uint8_t* x, const float* x_sca
  * unrounded values.  Sums are taken in an order that depends on the sizes, the activation and which of dx and dW are asked
  * for alone (together they may share a launch, cut into other parts).
  * in : dy [T,n_out]; pre [T,n_out] of the forward call and dp [T,n_out], scratch that is overwritten (both NULL
- *      with UNIPOOL_ACT_NONE; dp may be pre or dy); x, W of the forward call (x is needed for dW, W for dx);
- *      dx_residual [T,n_in] or NULL; scratch: unipool_linear_bwd_scratch() bytes of device memory, 16-byte aligned,
+ *      with UNIPOOL_ACT_NONE; dp may be pre or dy, not x or W); x, W of the forward call (x is needed for dW, W for dx);
+ *      dx_residual [T,n_in] or NULL (dp may lie on it too, as where both are dy: it is then copied into dx first, which
+ *      is neither dy nor pre in that call); scratch: unipool_linear_bwd_scratch() bytes of device memory, 16-byte aligned,
  *      which the call may use until it is complete on the stream (may be NULL where that is 0, or dW and dbias are NULL):
  *      for these T, n_in and n_out, since fewer tokens may be cut into more parts.
  * out: dx [T,n_in] (ctx dtype, overwritten; may be dx_residual, not an operand of the products: dp, dy with

@@ -514,6 +514,8 @@ int unipool_linear_bwd(unipool_ctx* ctx, const void* dy, int32_t T, int32_t n_ou
   if (dx != nullptr) CHECK_PTR(W);
   UP_REQUIRE(T == 0 || dx == nullptr || (dx != (act != UNIPOOL_ACT_NONE ? dp : dy) && (dW == nullptr || dx != x)), UNIPOOL_ERR_INVALID_ARG,
              "dx is an operand of the products: dp (dy without an activation), or x");
+  UP_REQUIRE(T == 0 || act == UNIPOOL_ACT_NONE || dx == nullptr || dx_residual != dp || (dx != dy && dx != pre), UNIPOOL_ERR_INVALID_ARG,
+             "dp lies on dx_residual, and dx, which would keep that, on dy or pre");
   // (its size, which takes a search, only where it decides)
   if ((dW != nullptr || dbias != nullptr) && T > 0 && (scratch == nullptr || (reinterpret_cast<uintptr_t>(scratch) & 15) != 0) &&
       linear_bwd_scratch(ctx, T, n_in, n_out) > 0)

@@ -423,7 +423,8 @@ size_t linear_bwd_scratch(const unipool_ctx* ctx, int T, int n_in, int n_out) {
   return (db_parts(ctx, T, n_out) + dw_parts(splits, n_in, n_out)) * sizeof(float);
 }
 
-int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) {
+int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& args, cudaStream_t s) {
+  LinearBwdArgs a = args;
   if (a.T == 0) {
     if (a.overwrite && a.dW != nullptr) UP_CUDA(cudaMemsetAsync(a.dW, 0, (size_t)a.n_in * a.n_out * sizeof(float), s));
     if (a.overwrite && a.dbias != nullptr) UP_CUDA(cudaMemsetAsync(a.dbias, 0, (size_t)a.n_out * sizeof(float), s));
@@ -435,6 +436,10 @@ int linear_bwd_launch(unipool_ctx* ctx, const LinearBwdArgs& a, cudaStream_t s) 
   PartSum<float> dW{}, db{};                             // what is left to add up
   // (few rows of dy itself are added up beside dW's parts: one launch less)
   const bool dy_rows = !act && a.dbias != nullptr && a.T <= kDyRows;
+  if (act && a.dx != nullptr && a.dx_residual == a.dp) {   // (x + act(x W^T): both dy) dp overwrites what dx still adds
+    UP_CUDA(cudaMemcpyAsync(a.dx, a.dx_residual, (size_t)a.T * a.n_in * ctx->elem_bytes, cudaMemcpyDeviceToDevice, s));
+    a.dx_residual = a.dx;
+  }
   if (act || (a.dbias != nullptr && !dy_rows)) {
     int blocks = 1;
     rc = tc ? dp_as<__nv_bfloat16, 8, true>(ctx, a, &blocks, a.scratch, s)

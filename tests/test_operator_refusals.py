@@ -206,3 +206,15 @@ def test_no_tokens_need_no_arrays_of_tokens(lib, ctx):
     for name, args in (("rmsnorm", norm), ("rmsnorm_bwd", back), ("linear", linear), ("linear_bwd", grad)):
         assert call(lib, name, args, T=1) == ARG and call(lib, name, args, T=-1) == ARG, name
     assert call(lib, "quantize_rows", rows, rows=1) == ARG
+
+
+def test_dp_over_the_residual_of_dx(lib, ctx):
+    """The residual is kept in dx, which must not be what dp is formed from."""
+    a = dict(ctx=ctx, dy=P, T=10, n_out=128, pre=2 * P, act=2, x=4 * P, n_in=128, W=5 * P, dp=P, dx_residual=P, dx=3 * P, dW=6 * P,
+             dbias=P, scratch=P, flags=0, stream=None)
+    f = lambda **c: call(lib, "linear_bwd", a, **c)
+    for c in ({}, dict(dp=2 * P), dict(dp=2 * P, dx_residual=2 * P), dict(dx=2 * P, dx_residual=3 * P), dict(act=0, dp=None, pre=None),
+              dict(dx=2 * P, T=0)):
+        assert f(**c) == 0, c
+    for c in (dict(dx=2 * P), dict(dx=P, dp=2 * P, dx_residual=2 * P)):
+        assert f(**c) == ARG and b"dx_residual" in lib.unipool_last_error(), c
