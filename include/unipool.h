@@ -403,7 +403,9 @@ int unipool_quantize_rows(unipool_ctx* ctx, const void* x, int32_t rows, int32_t
 /* Dense product with its epilogue, for the layers beside the experts (projections, dense FFN layers):
  *   p = x W^T + bias,  y = act(p) + residual,
  * accumulated in fp32, each output rounded once.  n_in and n_out are multiples of 64 up to 2^21, independent of d_model and
- * d_ff.
+ * d_ff.  In a bf16 context the tensor core truncates what it adds up, which costs sums of one sign up to 7e-9 of themselves per
+ * term; longer contractions than 16384 terms (in 8 bits 32768; up to four times that where tokens are few) are added up from
+ * parts of so many with rounding to nearest, so that no more than 1e-4 (5e-4) is lost.
  * in : x [T,n_in]; W [n_out,n_in] (ctx dtype); bias [n_out] float or NULL; act UNIPOOL_ACT_*; residual [T,n_out]
  *      (ctx dtype) or NULL.
  * out: y [T,n_out] (ctx dtype; may be residual); pre [T,n_out] (ctx dtype; p, which the backward call of an

@@ -37,10 +37,13 @@ constexpr int kLinEpiWarps = 16;
 constexpr int kLinThreads = 64 + 32 * kLinEpiWarps;
 constexpr int kLinChunk = 32;                            // columns that an epilogue warp has in hand
 constexpr uint32_t kLinTile = 32 * kLinChunk * 2;        // a chunk of 32 rows in bf16, rows of 64 bytes
-// The tensor core truncates the sums it adds to: a sum over K terms loses 1.1e-9 K of itself (measured, 512 to 32768 rows).  The
-// weight gradient, an fp32 result of a sum over all tokens, is therefore taken from the accumulator every 768 tokens and
-// added up in registers, where it is rounded to nearest.
+// The tensor core truncates the sums it adds to: over K terms of both signs they lose 1.1e-9 K of their magnitude (measured, 512 to 32768
+// rows), over terms of one sign 5e-9 to 7e-9 K in bf16 (16384 to 1048576), which at 262144 is a third of half a bf16 step and at
+// 2097152 three of them.  The weight gradient, an fp32 result of a sum over all tokens, is therefore taken from the accumulator every
+// 768 tokens and added up in registers, where it is rounded to nearest; the other products every 16384 terms (32768 in 8 bits), which
+// leaves 1e-4 at most and costs contractions of up to so many nothing.
 constexpr int kLinSegment = 12;                          // k-blocks of 64 tokens
+constexpr int kLinLong = 256;                            // k-blocks of 128 bytes
 
 struct LinearGrid {
   int M, N;                          // rows and columns of the result
@@ -142,8 +145,9 @@ __device__ __forceinline__ void activate(float (&v)[32], int act) {
 // kRes: a residual is added.  All of it is asked for before the accumulator is waited for: the first chunk's comes by TMA into
 // the staging tile, the second's into registers (a second tile for it would take an operand stage: 16384 tokens, 2048 -> 768 48.7
 // us instead of 44.8).  kPre: the value before the activation is stored too (one kernel with and without it where no residual is).
-// kN: columns of a tile, 256 or 128.
-template <int KIND, int kN, bool kRes, bool kPre>
+// kN: columns of a tile, 256 or 128.  kLong: a contraction of several parts of kLinLong k-blocks (a kernel of its own: the parts' sums and the branch
+// cost the others up to 5 %, 9001 tokens 1536 -> 4096 in e4m3 67.8 us instead of 66.2).
+template <int KIND, int kN, bool kRes, bool kPre, bool kLong>
 __global__ void __cluster_dims__(2, 1, 1) __launch_bounds__(kLinThreads, 1)
 linear_pair_kernel(const __grid_constant__ LinearMaps m, LinearParams p) {
   constexpr uint32_t kStage = kLinHalf + kN * 64;         // 128 rows of A, kN / 2 of B
@@ -233,7 +237,7 @@ linear_pair_kernel(const __grid_constant__ LinearMaps m, LinearParams p) {
         const uint32_t idesc = KIND == kLinFwd8 ? tc::instr_desc_e4m3(kN, 256) : tc::instr_desc_bf16(kN, a_mn, kBMn, 256);
         const uint32_t a_lbo = a_mn ? kLinHalf / 2 : 16, a_step = (a_mn ? 16 * 128 : 32) >> 4;
         for (int kb = t.kb0; kb < t.kb1 && ok;) {
-          const int end = a_mn ? min(t.kb1, kb + kLinSegment) : t.kb1;
+          const int end = a_mn ? min(t.kb1, kb + kLinSegment) : kLong ? min(t.kb1, kb + kLinLong) : t.kb1;
           const int acc = local & 1;
           if (!tc::mbar_wait(&tmem_empty[acc], ((local >> 1) & 1) ^ 1u, abort)) { linear_timeout(p.status, abort, 42); ok = false; break; }
           ++local;
@@ -331,7 +335,6 @@ linear_pair_kernel(const __grid_constant__ LinearMaps m, LinearParams p) {
         }
       }
       if (KIND != kLinDw && !(kBoth && dw)) {
-        const int acc = local & 1;
         const bool mine = row0 + lane < g.M;
         uint32_t r1[16];
         if constexpr (kRes) {
@@ -349,6 +352,26 @@ linear_pair_kernel(const __grid_constant__ LinearMaps m, LinearParams p) {
         }
         float xs = 1.f;
         if (KIND == kLinFwd8 && mine) xs = __ldg(p.x_scale + row0 + lane);
+        float held[kLong ? kPart : 1];                    // sums of the parts but the last (indexed by a variable: local memory, no registers)
+        if constexpr (kLong) {
+#pragma unroll 1
+          for (int kb = t.kb0; kb + kLinLong < t.kb1; kb += kLinLong) {
+            const int a = local & 1;
+            ok = wait_full(a);
+            if (!ok) break;
+#pragma unroll 1
+            for (int c = 0; c < kPart; c += 16) {
+              uint32_t rr[16];
+              tc::tmem_ld_32x16(tmem_base + lanes + a * 256 + part * kPart + c, rr);
+              tc::tmem_ld_wait();
+#pragma unroll
+              for (int i = 0; i < 16; ++i) held[c + i] = (kb > t.kb0 ? held[c + i] : 0.f) + __uint_as_float(rr[i]);
+            }
+            release(a);
+          }
+          if (!ok) break;
+        }
+        const int acc = local & 1;
         ok = wait_full(acc);
         if (!ok) break;
 #pragma unroll
@@ -366,6 +389,10 @@ linear_pair_kernel(const __grid_constant__ LinearMaps m, LinearParams p) {
           float v[32];
 #pragma unroll
           for (int i = 0; i < 32; ++i) v[i] = __uint_as_float(rr[i]);
+          if constexpr (kLong) {
+#pragma unroll
+            for (int i = 0; i < 32; ++i) v[i] += held[ch * kLinChunk + i];
+          }
           if constexpr (KIND == kLinFwd8) {
             if (kRes) c.load(p.w_scale + col, p.vec);
 #pragma unroll
@@ -454,11 +481,16 @@ LinearGrid linear_grid(int M, int N, int tile_n, int kb_total, int splits) {
 template <int KIND, int kN, bool kRes, bool kPre>
 int launch_linear(unipool_ctx* ctx, int phase, const LinearMaps& m, const LinearParams& p, cudaStream_t s) {
   PhaseTimer pt(ctx, phase, 1, s);
-  auto kern = linear_pair_kernel<KIND, kN, kRes, kPre>;
-  UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLinSmem));
-  const int pairs = ctx->sm_count / 2, units = p.g.units + p.w.units;
-  UP_KERNEL(kern, 2 * (units < pairs ? units : pairs), kLinThreads, kLinSmem, s, m, p);
-  return UNIPOOL_OK;
+  auto run = [&](auto kern) {
+    UP_CUDA(cudaFuncSetAttribute(kern, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)kLinSmem));
+    const int pairs = ctx->sm_count / 2, units = p.g.units + p.w.units;
+    UP_KERNEL(kern, 2 * (units < pairs ? units : pairs), kLinThreads, kLinSmem, s, m, p);
+    return (int)UNIPOOL_OK;
+  };
+  if constexpr (KIND != kLinDw) {
+    if (p.g.kb_split > kLinLong) return run(linear_pair_kernel<KIND, kN, kRes, kPre, true>);
+  }
+  return run(linear_pair_kernel<KIND, kN, kRes, kPre, false>);
 }
 
 template <typename... P> bool aligned(uintptr_t n, P... p) { return ((... | reinterpret_cast<uintptr_t>(p)) & (n - 1)) == 0; }
@@ -480,6 +512,7 @@ template <typename... P> bool aligned(uintptr_t n, P... p) { return ((... | rein
 // And every launch asks for so much shared memory that no more CTAs lie on an SM than it has columns for.
 constexpr int kFewTokens = 128, kFewMaxStages = 12;
 constexpr uint32_t kFewBars = 512;
+constexpr int kFewLong = 1024;                           // k-blocks of a CTA at most: 65536 terms in bf16, which lose 5e-4 at most (kLinSegment)
 constexpr uint32_t kFewColumns = 128;                    // of the SM's 512: one accumulator of up to 128 tokens
 constexpr uint32_t kFewSmemLeast = 46080;                // (with the system's 1 KB, five CTAs are more than an SM's 228 KB)
 static_assert(kFewColumns >= kFewTokens && (512 / kFewColumns + 1) * (kFewSmemLeast + 1024) > 228 * 1024, "tensor memory of an SM");
@@ -705,7 +738,8 @@ FormTime linear_form(const unipool_ctx* ctx, int M, int N, int kb, bool plain) {
     const FewShape f = few_shape(M, N, kb);
     const double ctas = (double)f.tiles * f.splits / ctx->sm_count, each = (kb + f.splits - 1) / f.splits * (16.0 + f.N / 8.0);
     const double few = 3.2 + (f.wide ? 0.02 : 0.03) * f.N + (ctas > 1.0 ? 1.7 + ctas * each / 120.0 : each / 85.0);
-    if (ctas <= 2.0 && few < p128 && few < p256) return {kFew, few};     // (several rounds of its CTAs never were the fastest)
+    // (several rounds of its CTAs never were the fastest; and one accumulator for all of a CTA's contraction)
+    if (ctas <= 2.0 && few < p128 && few < p256 && (kb + f.splits - 1) / f.splits <= kFewLong) return {kFew, few};
   }
   return p128 < p256 ? FormTime{kPairs128, p128} : FormTime{kPairs256, p256};
 }
