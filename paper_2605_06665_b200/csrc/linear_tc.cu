@@ -755,7 +755,11 @@ int few_as(unipool_ctx* ctx, int phase, const CUtensorMap& tmW, const CUtensorMa
   const uint32_t bytes = p.stages * stage > p.N * 512u ? p.stages * stage : p.N * 512u;   // the sums lie there too
   auto as = [&](auto e) {
     constexpr int E = decltype(e)::value;
-    auto run = splits == 8 ? launch_few<KIND, 8, E> : splits == 4 ? launch_few<KIND, 4, E> : splits == 2 ? launch_few<KIND, 2, E> : launch_few<KIND, 1, E>;
+    auto run = splits == 2 ? launch_few<KIND, 2, E> : launch_few<KIND, 1, E>;
+    if constexpr (E == 4) {                              // (few_shape takes sixteen warps for no more than two CTAs)
+      if (splits == 8) run = launch_few<KIND, 8, E>;
+      if (splits == 4) run = launch_few<KIND, 4, E>;
+    }
     return run(ctx, phase, tmW, tmX, p, std::max(2048 + bytes, kFewSmemLeast), s);
   };
   return f.wide ? as(std::integral_constant<int, 16>()) : as(std::integral_constant<int, 4>());

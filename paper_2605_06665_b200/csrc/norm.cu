@@ -501,7 +501,10 @@ template <bool kNorm, typename E> int norm_as(unipool_ctx* ctx, const NormParams
     if (n <= 256) return run(Int<V>(), Int<32>(), Int<8>());
     if (n <= 512) return run(Int<V>(), Int<128>(), Int<4>());
     if (n <= 1024) return run(Int<V>(), Int<256>(), Int<4>());
-    return n <= 2048 ? run(Int<V>(), Int<512>(), Int<4>()) : run(Int<V>(), Int<512>(), Int<8>());
+    if constexpr (V == 4) {                              // (no row has more than 2048 vectors of eight)
+      if (n > 2048) return run(Int<V>(), Int<512>(), Int<8>());
+    }
+    return run(Int<V>(), Int<512>(), Int<4>());
   }
   auto narrow = [&](auto v) {
     const int n = p.width / decltype(v)::value;
@@ -530,7 +533,10 @@ int norm_bwd_run(const NormBwdShape& f, const NormBwdParams& p, cudaStream_t s) 
     UP_KERNEL(kern, C > 1 ? C : f.blocks, f.threads, f.smem > sums ? f.smem : sums, s, p);
     return (int)UNIPOOL_OK;
   };
-  return f.cluster ? run(std::integral_constant<int, kNormBwdCluster>()) : run(std::integral_constant<int, 1>());
+  if constexpr (VPT <= 8) {                              // (norm_bwd_shape takes no cluster for more)
+    if (f.cluster) return run(std::integral_constant<int, kNormBwdCluster>());
+  }
+  return run(std::integral_constant<int, 1>());
 }
 
 template <typename E> int norm_bwd_as(unipool_ctx* ctx, NormBwdParams p, bool aligned, float* scratch, bool overwrite, cudaStream_t s) {
