@@ -334,6 +334,7 @@ typedef struct {
   void *dYp, *dGU, *dx;                      /* dx [2,T,d]: dx[0] holds the upstream gradient on entry of     */
                                              /* backward, dx[n_layers % 2] the gradient of x[0] on return     */
   float *dgate, *dW_gu, *dW_down, *dW_r, *dsigma;
+  /* (Up to here the struct that programs were built with before it had norms.)                                      */
   /* Pre-normalised blocks, x_{l+1} = x_l + MoE_l(norm(x_l)) with unipool_rmsnorm of every layer's own weight: W_n not   */
   /* NULL.  Everything of the layer, the saved activations too, then works on h in the place of x.                       */
   const float* W_n;                          /* [L,d]                                                        */
@@ -358,6 +359,16 @@ int unipool_stack_aux_loss(unipool_ctx* ctx, const unipool_stack* stack, int32_t
  * add), UNIPOOL_STACK_NO_AUX, UNIPOOL_STACK_LEAVE_WGRAD. */
 int unipool_stack_backward(unipool_ctx* ctx, const unipool_stack* stack, int32_t T, int32_t flags,
                            unipool_stream stream);
+/* The same, told how many bytes of the struct the caller knows: fields beyond them are NULL or 0.  The calls above,
+ * which programs built before the struct had norms were linked against, read the fields up to dsigma; in programs
+ * built with this header they are the calls that are told. */
+int unipool_stack_forward_sized(unipool_ctx* ctx, const unipool_stack* stack, size_t stack_bytes, int32_t T,
+                                unipool_stream stream);
+int unipool_stack_backward_sized(unipool_ctx* ctx, const unipool_stack* stack, size_t stack_bytes, int32_t T, int32_t flags,
+                                 unipool_stream stream);
+#define unipool_stack_forward(ctx, stack, T, stream) unipool_stack_forward_sized(ctx, stack, sizeof(unipool_stack), T, stream)
+#define unipool_stack_backward(ctx, stack, T, flags, stream) \
+  unipool_stack_backward_sized(ctx, stack, sizeof(unipool_stack), T, flags, stream)
 
 /* RMS norm of the residual stream with the addition in front of it (the pre-normalised block of the LLaMA-style
  * backbone, App. B, App. D), for rows of any width from 1 to 16384:
@@ -484,6 +495,11 @@ enum {
 };
 int unipool_profile_enable(unipool_ctx* ctx, int32_t on);
 int unipool_profile_read(unipool_ctx* ctx, double* ms, int64_t* launches);
+/* The same into arrays of n_phases entries (phases beyond them are forgotten).  unipool_profile_read itself, which
+ * programs built before there were norms and dense products were linked against, writes the phases up to
+ * UNIPOOL_PH_ROUTE_BWD_DW; in programs built with this header it is the call that is told. */
+int unipool_profile_read_n(unipool_ctx* ctx, int32_t n_phases, double* ms, int64_t* launches);
+#define unipool_profile_read(ctx, ms, launches) unipool_profile_read_n(ctx, UNIPOOL_N_PHASES, ms, launches)
 
 /* Name of the kernel that a grouped-GEMM phase of this context runs for a router of n_experts experts, with
  * (sizes_known != 0) or without the group sizes; "" for other phases (host function, a measurement aid). */

@@ -33,6 +33,7 @@ EXPORTS = (
     "unipool_gemm_kernel", "unipool_dispatch_rows", "unipool_expert_fwd_rows", "unipool_expert_bwd_rows", "unipool_pool_wgrad_rows",
     "unipool_rmsnorm", "unipool_rmsnorm_bwd", "unipool_rmsnorm_bwd_scratch", "unipool_quantize_rows",
     "unipool_linear", "unipool_linear_scaled", "unipool_linear_bwd", "unipool_linear_bwd_scratch",
+    "unipool_stack_forward_sized", "unipool_stack_backward_sized", "unipool_profile_read_n",
 )
 
 PHASES = (
@@ -132,6 +133,10 @@ def lib():
     L.unipool_stack_aux_loss.argtypes = [vp, stackp, i32, f32, vp, vp]
     L.unipool_stack_backward.restype = ctypes.c_int
     L.unipool_stack_backward.argtypes = [vp, stackp, i32, i32, vp]
+    L.unipool_stack_forward_sized.restype = ctypes.c_int
+    L.unipool_stack_forward_sized.argtypes = [vp, stackp, ctypes.c_size_t, i32, vp]
+    L.unipool_stack_backward_sized.restype = ctypes.c_int
+    L.unipool_stack_backward_sized.argtypes = [vp, stackp, ctypes.c_size_t, i32, i32, vp]
     L.unipool_gemm_kernel.restype = ctypes.c_char_p
     L.unipool_gemm_kernel.argtypes = [vp, i32, i32, i32]
     L.unipool_unique_experts.restype = ctypes.c_int
@@ -160,6 +165,8 @@ def lib():
     L.unipool_profile_enable.argtypes = [vp, i32]
     L.unipool_profile_read.restype = ctypes.c_int
     L.unipool_profile_read.argtypes = [vp, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i64)]
+    L.unipool_profile_read_n.restype = ctypes.c_int
+    L.unipool_profile_read_n.argtypes = [vp, i32, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(i64)]
     _lib = L
     return L
 
@@ -300,13 +307,13 @@ class Context:
                                        _p(dsigma), _stream()))
 
     def stack_forward(self, stack, T):
-        _check(lib().unipool_stack_forward(self.handle, ctypes.byref(stack), T, _stream()))
+        _check(lib().unipool_stack_forward_sized(self.handle, ctypes.byref(stack), ctypes.sizeof(stack), T, _stream()))
 
     def stack_aux_loss(self, stack, T, alpha, fbar_prev=None):
         _check(lib().unipool_stack_aux_loss(self.handle, ctypes.byref(stack), T, alpha, _p(fbar_prev), _stream()))
 
     def stack_backward(self, stack, T, flags=0):
-        _check(lib().unipool_stack_backward(self.handle, ctypes.byref(stack), T, flags, _stream()))
+        _check(lib().unipool_stack_backward_sized(self.handle, ctypes.byref(stack), ctypes.sizeof(stack), T, flags, _stream()))
 
     # ---- the operators around the MoE layer
     def rmsnorm(self, x, y, T, width, w, eps, r, rstd, h, q=None, q_scale=None):
@@ -376,7 +383,7 @@ class Context:
         n = len(PHASES)
         ms = (ctypes.c_double * n)()
         launches = (ctypes.c_int64 * n)()
-        _check(lib().unipool_profile_read(self.handle, ms, launches))
+        _check(lib().unipool_profile_read_n(self.handle, n, ms, launches))
         return {PHASES[i]: (float(ms[i]), int(launches[i])) for i in range(n)}
 
     def gemm_kernel(self, phase, n_experts, sizes_known=True):

@@ -211,20 +211,28 @@ int unipool_profile_enable(unipool_ctx* ctx, int32_t on) {
   return UNIPOOL_OK;
 }
 
-int unipool_profile_read(unipool_ctx* ctx, double* ms, int64_t* launches) {
+int unipool_profile_read_n(unipool_ctx* ctx, int32_t n_phases, double* ms, int64_t* launches) {
   CHECK_CTX(ctx); CHECK_PTR(ms); CHECK_PTR(launches);
-  for (int i = 0; i < UNIPOOL_N_PHASES; ++i) { ms[i] = 0.0; launches[i] = 0; }
+  UP_REQUIRE(n_phases >= 0, UNIPOOL_ERR_INVALID_ARG, "n_phases = %d is negative", n_phases);
+  for (int i = 0; i < n_phases; ++i) { ms[i] = 0.0; launches[i] = 0; }
   for (const ProfRecord& r : ctx->prof.records) {
     UP_CUDA(cudaEventSynchronize(r.stop));
     float t = 0.f;
     UP_CUDA(cudaEventElapsedTime(&t, r.start, r.stop));
-    ms[r.phase] += t;
-    launches[r.phase] += r.launches;
+    if (r.phase < n_phases) {
+      ms[r.phase] += t;
+      launches[r.phase] += r.launches;
+    }
     ctx->prof.free_events.push_back(r.start);
     ctx->prof.free_events.push_back(r.stop);
   }
   ctx->prof.records.clear();
   return UNIPOOL_OK;
+}
+
+// (the name in parentheses: the symbol, not the header's macro)
+int (unipool_profile_read)(unipool_ctx* ctx, double* ms, int64_t* launches) {
+  return unipool_profile_read_n(ctx, UNIPOOL_PH_ROUTE_BWD_DW + 1, ms, launches);
 }
 
 const char* unipool_gemm_kernel(const unipool_ctx* ctx, int32_t phase, int32_t n_experts, int32_t sizes_known) {

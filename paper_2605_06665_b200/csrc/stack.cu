@@ -2,6 +2,8 @@
 // A pass of twelve layers is some sixty calls forward and a hundred backward; issued one by one through a
 // Python binding they cost the host 13 us each (argument conversion, tensor slicing), more than the kernels of
 // a small batch take.
+#include <cstddef>
+#include <cstring>
 #include <type_traits>
 
 #include "common.cuh"
@@ -59,8 +61,20 @@ int check_stack(const unipool_ctx* ctx, const unipool_stack* s) {
   UP_REQUIRE(s->n_layers >= 1 && s->n_layers <= ctx->cfg.n_layers && s->layers_per_group >= 1 &&
                  s->n_layers % s->layers_per_group == 0,
              UNIPOOL_ERR_INVALID_ARG, "stack of %d layers in groups of %d", s->n_layers, s->layers_per_group);
-  UP_REQUIRE(s->W_n == nullptr || (s->h != nullptr && s->rstd != nullptr), UNIPOOL_ERR_INVALID_ARG, "W_n without h or rstd");
   UP_REQUIRE(s->sigma != nullptr && s->x != nullptr, UNIPOOL_ERR_INVALID_ARG, "sigma or x is NULL");
+  return UNIPOOL_OK;
+}
+
+// The caller's struct, of which it knows `bytes`, in one of ours.
+constexpr size_t kStackLeast = offsetof(unipool_stack, W_n);
+int take_stack(const unipool_ctx* ctx, const unipool_stack* s, size_t bytes, unipool_stack* out) {
+  UP_REQUIRE(ctx != nullptr && s != nullptr, UNIPOOL_ERR_INVALID_ARG, "ctx or stack is NULL");
+  UP_REQUIRE(bytes >= kStackLeast && bytes <= sizeof(unipool_stack), UNIPOOL_ERR_INVALID_ARG,
+             "a stack of %zu bytes, this library knows those of %zu to %zu", bytes, kStackLeast, sizeof(unipool_stack));
+  std::memset(out, 0, sizeof *out);
+  std::memcpy(out, s, bytes);
+  UP_TRY(check_stack(ctx, out));
+  UP_REQUIRE(out->W_n == nullptr || (out->h != nullptr && out->rstd != nullptr), UNIPOOL_ERR_INVALID_ARG, "W_n without h or rstd");
   return UNIPOOL_OK;
 }
 
@@ -85,8 +99,10 @@ int permute_and_experts(unipool_ctx* ctx, const Layer& a, int32_t T, int w, unip
 
 extern "C" {
 
-int unipool_stack_forward(unipool_ctx* ctx, const unipool_stack* s, int32_t T, unipool_stream stream) {
-  UP_TRY(check_stack(ctx, s));
+int unipool_stack_forward_sized(unipool_ctx* ctx, const unipool_stack* stack, size_t stack_bytes, int32_t T, unipool_stream stream) {
+  unipool_stack known;
+  UP_TRY(take_stack(ctx, stack, stack_bytes, &known));
+  const unipool_stack* s = &known;
   // The terms of all routers, for this pass and the backward pass that follows it; few tokens read the weights themselves, so
   // no copy is kept beside the terms (8.2 us instead of 10.2 for twelve routers of 96 x 768).
   struct Now {
@@ -116,8 +132,11 @@ int unipool_stack_aux_loss(unipool_ctx* ctx, const unipool_stack* s, int32_t T, 
   return UNIPOOL_OK;
 }
 
-int unipool_stack_backward(unipool_ctx* ctx, const unipool_stack* s, int32_t T, int32_t flags, unipool_stream stream) {
-  UP_TRY(check_stack(ctx, s));
+int unipool_stack_backward_sized(unipool_ctx* ctx, const unipool_stack* stack, size_t stack_bytes, int32_t T, int32_t flags,
+                                 unipool_stream stream) {
+  unipool_stack known;
+  UP_TRY(take_stack(ctx, stack, stack_bytes, &known));
+  const unipool_stack* s = &known;
   UP_REQUIRE((flags & ~(UNIPOOL_WGRAD_OVERWRITE | UNIPOOL_STACK_NO_AUX | UNIPOOL_STACK_LEAVE_WGRAD)) == 0,
              UNIPOOL_ERR_INVALID_ARG, "unknown flags 0x%x", flags);
   UP_REQUIRE(s->wgrad_layers >= 1 && s->dx != nullptr, UNIPOOL_ERR_INVALID_ARG, "wgrad_layers = %d, or dx is NULL",
@@ -165,6 +184,14 @@ int unipool_stack_backward(unipool_ctx* ctx, const unipool_stack* s, int32_t T, 
                                    s->dW_gu, s->dW_down, overwrite, stream));
   }
   return UNIPOOL_OK;
+}
+
+// (the names in parentheses: the symbols, not the header's macros)
+int (unipool_stack_forward)(unipool_ctx* ctx, const unipool_stack* stack, int32_t T, unipool_stream stream) {
+  return unipool_stack_forward_sized(ctx, stack, kStackLeast, T, stream);
+}
+int (unipool_stack_backward)(unipool_ctx* ctx, const unipool_stack* stack, int32_t T, int32_t flags, unipool_stream stream) {
+  return unipool_stack_backward_sized(ctx, stack, kStackLeast, T, flags, stream);
 }
 
 }  // extern "C"
