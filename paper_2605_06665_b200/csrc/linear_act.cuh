@@ -1,5 +1,5 @@
-// Activations of the dense products and their derivatives.  kFast: through the special-function unit (errors of a few
-// 2^-22, far below the rounding to bf16); otherwise CUDA's expf and divisions.
+// Activations of the dense products and their derivatives.  kFast: through the special-function unit (errors of a few 2^-22, gelu's slope
+// 2^-18, far below the rounding to bf16); otherwise CUDA's expf and divisions.
 #pragma once
 
 #include "common.cuh"
@@ -34,19 +34,38 @@ template <bool kFast> __device__ __forceinline__ float act_value(float p, int ac
   }
 }
 
+// The logistic function and what it lacks to 1, both to fp32's relative accuracy (1 - s where s nears 1 would keep its absolute error of 2^-25 only,
+// which gelu's slope multiplies by 40: 2e-6 at 5).
+struct Logistic { float s, rest; };
+__device__ __forceinline__ Logistic logistic_both(float a) {
+  const float e = expf(-fabsf(a)), r = 1.f / (1.f + e), er = e * r;
+  return a >= 0.f ? Logistic{r, er} : Logistic{er, r};
+}
+
 template <bool kFast> __device__ __forceinline__ float act_slope(float p, int act) {
   switch (act) {
     case UNIPOOL_ACT_RELU: return p > 0.f ? 1.f : p <= 0.f ? 0.f : p;
     case UNIPOOL_ACT_SILU: {
-      const float s = logistic<kFast>(p);
-      return s * (1.f + p * (1.f - s));
+      if constexpr (kFast) {
+        const float s = logistic<true>(p);
+        return s * (1.f + p * (1.f - s));
+      } else {
+        const Logistic l = logistic_both(p);
+        return l.s * (1.f + p * l.rest);
+      }
     }
     case UNIPOOL_ACT_GELU: {
       const float q = fminf(fmaxf(p, -30.f), 30.f), q2 = q * q;     // 0 or 1 from there on; the square would overflow
-      float s;                                                      // (p itself carries a NaN into s)
-      if constexpr (kFast) s = rcp_1_ex2(p * fmaf(q2, -kLog2e * kGeluTwice * kGeluCube, -kLog2e * kGeluTwice));
-      else s = logistic<false>(kGeluTwice * (p + kGeluCube * p * q2));
-      return fmaf(fmaf(-s, s, s), q * fmaf(q2, 3.f * kGeluTwice * kGeluCube, kGeluTwice), s);
+      float s, both;                                                // s (1 - s); (p itself carries a NaN into s)
+      if constexpr (kFast) {
+        s = rcp_1_ex2(p * fmaf(q2, -kLog2e * kGeluTwice * kGeluCube, -kLog2e * kGeluTwice));
+        both = fmaf(-s, s, s);
+      } else {
+        const Logistic l = logistic_both(kGeluTwice * (p + kGeluCube * p * q2));
+        s = l.s;
+        both = l.s * l.rest;
+      }
+      return fmaf(both, q * fmaf(q2, 3.f * kGeluTwice * kGeluCube, kGeluTwice), s);
     }
     default: return 1.f;
   }
