@@ -22,7 +22,9 @@
  *   - Tensors are dense row-major; shapes are written [rows, cols].
  *   - Calls are asynchronous on `stream` and never synchronise the host: group
  *     sizes stay on the device.  Calls of one context must be issued on one
- *     stream at a time (they share the workspace).
+ *     stream at a time (they share the workspace); only those of the norm and of
+ *     the dense products, which use none of it but the status word, may run on
+ *     several at once, beside the others too, each with scratch of its own.
  *   - unipool_rmsnorm, unipool_linear and the calls beside them take no tokens too: T (or rows) = 0 leaves every array of
  *     that dimension alone, and those may be NULL.
  *   - Arguments marked "+=" accumulate into what the buffer holds.
@@ -373,7 +375,8 @@ int unipool_stack_backward_sized(unipool_ctx* ctx, const unipool_stack* stack, s
 /* RMS norm of the residual stream with the addition in front of it (the pre-normalised block of the LLaMA-style
  * backbone, App. B, App. D), for rows of any width from 1 to 16384:
  *   r = x + y;  n_t = 1 / sqrt(mean_j r_tj^2 + eps);  h = r * n_t * w;
- *   q = e4m3(h / s_t) with s_t = max(max_j |h_tj| / 448, 2^-126), rounded to nearest even.
+ *   q = e4m3(h / s_t) with s_t = max(max_j |h_tj| / 448, 2^-126), rounded to nearest even (as h times 1 / s_t in fp32: a
+ *   quotient within 2^-22 of itself of the middle between two values may go to either).
  * The statistics are fp32 and h is formed from the unrounded sum; each output is rounded once.  A row that holds
  * a NaN has NaN in rstd, h, q and q_scale; infinities follow the formulas, as do sums of squares that pass fp32's
  * range (rstd 0).  With eps = 0 a row of zeros has no norm (NaN).
@@ -393,7 +396,8 @@ int unipool_rmsnorm(unipool_ctx* ctx, const void* x, const void* y, int32_t T, i
  *      enough for fewer rows of that width.
  * out: dx [T,width] (ctx dtype, overwritten; may be dh, r or dr); dw [width] float +=, or NULL.
  * flags: 0 or UNIPOOL_WGRAD_OVERWRITE (dw is written, not added to).  The sums over the rows are taken in an order
- * that depends on T and width alone. */
+ * that depends on T, width, the element type, whether dr is given, whether all arrays lie on 16 bytes, and the GPU's number
+ * of SMs: the same call gives the same bits, one with dr may add up dw otherwise than one without. */
 int unipool_rmsnorm_bwd(unipool_ctx* ctx, const void* dh, const void* r, int32_t T, int32_t width, const float* w,
                         const float* rstd, const void* dr, void* dx, float* dw, void* scratch, int32_t flags,
                         unipool_stream stream);
@@ -436,8 +440,9 @@ int unipool_linear_scaled(unipool_ctx* ctx, const uint8_t* x, const float* x_sca
 /* Backward of unipool_linear:
  *   dp = dy act'(p);  dx = dp W (+ dx_residual);  dW += dp^T x;  dbias += sum_t dp
  * (the residual's gradient is dy).  dp is rounded to the ctx dtype, as an operand of both products; dbias sums the
- * unrounded values.  Sums are taken in an order that depends on the sizes, the activation and which of dx and dW are asked
- * for alone (together they may share a launch, cut into other parts).
+ * unrounded values.  Sums are taken in an order that depends on the sizes, the activation, which of dx and dW are asked
+ * for (together they may share a launch, cut into other parts) and the GPU's number of SMs; in an fp32 context that of dbias
+ * also on whether dy, pre and dp lie on 16 bytes.
  * in : dy [T,n_out]; pre [T,n_out] of the forward call and dp [T,n_out], scratch that is overwritten (both NULL
  *      with UNIPOOL_ACT_NONE; dp may be pre or dy, not x or W); x, W of the forward call (x is needed for dW, W for dx);
  *      dx_residual [T,n_in] or NULL (dp may lie on it too, as where both are dy: it is then copied into dx first, which

@@ -11,9 +11,13 @@
 // waits (tensor memory, shared memory, proxy fence, TMA) of a microsecond, which it takes four warps on a scheduler to hide behind
 // the products of 768 inputs, the special-function unit (two instructions an element of silu and gelu) being busy for 2.2 of
 // the 3.1 us that they take.
-// Bound by the tensor pipe (operands through shared memory; see expert_tc.cu) and, held for long, by power: 9001 tokens 1536 -> 4096 79 us
-// (1.44 PFLOP/s), in e4m3 50 us (2.28 PFLOP/s), 16384 tokens 768 -> 2048 42 us, with gelu 46, with p stored too 52.  With few tiles of a long
-// contraction by what the L2 delivers (1501 tokens 4096 -> 1536: 72 tiles of 256 x 128, 26 us).
+// Long contractions of many tokens are bound by the tensor pipe (operands through shared memory; see expert_tc.cu) and, held for long, by power:
+// 32768 tokens 4096 -> 1536 345 us (1.2 PFLOP/s held), 9001 tokens 1536 -> 4096 79 us (1.44 PFLOP/s).  Short ones, and 8 bits, whose products
+// take half the time, by the epilogue (the pipe 56 % busy in both): 9001 tokens 1536 -> 4096 in e4m3 50 us (2.28 PFLOP/s), 56 to 66 with bias and silu;
+// 16384 tokens 768 -> 2048 42 us, with gelu 46, with p stored too 52 to 61.  Few tiles of a long contraction by what the L2
+// delivers (1501 tokens 4096 -> 1536: 72 tiles of 256 x 128, 26 us).
+// 18 warps leave 96 registers to a thread, and some of them spill: dx beside dW with a residual on 256 columns 76 bytes stored and 140 loaded a
+// thread, the forward ones up to 36 and 48; the times above are with that.
 #include <cuda.h>
 
 #include <algorithm>

@@ -7,8 +7,9 @@
 //
 // Bound by HBM: forward 2 (x, h) to 4 (y, r too) passes over the stream, backward 3 to 4, next to no arithmetic.  A row stays
 // in the registers of the threads that share it, so that it is read once: a warp up to 256 vectors of 16 bytes (2048 bf16
-// columns), four or sixteen warps beyond; all of a thread's loads are issued before the first is used.  Rows whose bytes are no
-// multiple of 16, and misaligned tensors, go two elements or one at a time through the same kernels.  16384 x 768 bf16 with residual 17 us
+// columns), four, eight or sixteen beyond; all of a thread's loads are issued before the first is used.  Rows whose bytes are no
+// multiple of 16, and misaligned tensors, go two elements or one at a time through the same kernels (one, four, five, eight, ten or sixteen
+// warps to a row).  16384 x 768 bf16 with residual 17 us
 // (5.9 TB/s), 32768 x 1536 with 8 bits too 71 us (6.4 TB/s); backward of 16384 x 768 with dr 22 us, 4 of them for adding up dw.
 // Sums of squares, the statistics and the gradient of w are fp32; h is formed from the unrounded sum r.
 #include <cooperative_groups.h>
@@ -214,7 +215,7 @@ template <int R> __device__ __forceinline__ int row_of_lane(int lane) { return l
 // shared memory some stages ahead, so that reads go on while rows are worked on and whatever the rows' alignment (16384 rows of
 // 770 bf16 read element by element 69 us, through the ring 35).  Without it (arrays off 16 bytes, rows too long for two stages) the loads go
 // from memory into registers.
-// The sums' order depends on the sizes alone.  C > 1: the blocks are one cluster, which adds its sums for dw up through each other's shared
+// The sums' order depends on the sizes, the number of arrays and their alignment (norm_bwd_shape).  C > 1: the blocks are one cluster, which adds its sums for dw up through each other's shared
 // memory, in the order of the ranks.
 template <typename E, int V, int VPT, int R, bool kRing, int C>
 __global__ void __cluster_dims__(C, 1, 1) __launch_bounds__(512, V * sizeof(E) == 16 ? 1 : 2) rmsnorm_bwd_kernel(NormBwdParams p) {
@@ -564,7 +565,7 @@ template <typename E> int norm_bwd_as(unipool_ctx* ctx, NormBwdParams p, bool al
   int rc;
   if (f.stages > 0) rc = f.v == V ? by_vpt(Int<V>(), std::true_type()) : f.v == 1 ? by_vpt(Int<1>(), std::true_type()) : by_vpt(Int<2>(), std::true_type());
   else if (f.v == 1) rc = by_vpt(Int<1>(), std::false_type());
-  else if constexpr (V == 4) rc = norm_bwd_run<E, 4, 8, false>(f, p, s);   // fp32 rows of 9472 and more: two do not fit
+  else if constexpr (V == 4) rc = norm_bwd_run<E, 4, 8, false>(f, p, s);   // fp32 rows of 9288 and more with dr, 13936 without: two do not fit
   else rc = UNIPOOL_ERR_UNSUPPORTED;                     // (every bf16 row's do)
   return rc == UNIPOOL_OK && split ? column_sum_launch(scratch, f.blocks, p.width, dw, !overwrite, s) : rc;
 }
