@@ -68,3 +68,49 @@ def test_many_streams(ctx, recorded):
         for s, w in zip(sets, want):
             for (_, y, dx, _), (y0, dx0) in zip(s, w):
                 assert torch.equal(y, y0) and torch.equal(dx, dx0)
+
+
+def test_products_beside_a_stack_on_another_stream(ctx):
+    """Products of one context while a stack of pre-normalised blocks (another context, kernels that take whole SMs) runs its steps; and
+    products and norms of that stack's own context."""
+    from paper_2605_06665_b200.stack import UniPoolStack
+    T, d = 700, 256
+    st = UniPoolStack(3, d, 320, 12, 2, T, "bf16", c=1.7, norm=True)
+    g = torch.Generator(device="cpu").manual_seed(3)
+    draw = lambda t, std: t.copy_((torch.randn(t.shape, generator=g) * std).to(t.dtype))
+    draw(st.W_gu, 0.08), draw(st.W_down, 0.08), draw(st.W_r, 0.3)
+    x0, up = (torch.randn(T, d, generator=g).bfloat16().cuda() for _ in range(2))
+    names = ("x", "dW_n", "dW_gu", "dW_down", "rstd")
+    st.step(x0, up, accumulate=False)
+    want = [getattr(st, n).clone() for n in names]
+    own, w = calls(ctx, 77), torch.ones(d, device="cuda")
+    of_stack = calls(st.ctx, 78)[:2]
+    h, h0 = torch.empty_like(x0), torch.empty_like(x0)
+    st.ctx.rmsnorm(x0, None, T, d, w, 1e-6, None, None, h0)
+    for c, *_ in own + of_stack:
+        c()
+    torch.cuda.synchronize()
+    results = [(y.clone(), dx.clone()) for _, y, dx, _ in own + of_stack]
+    a, b, c = (torch.cuda.Stream() for _ in range(3))
+    for _ in range(10):
+        for n in names:
+            getattr(st, n)[:].zero_()
+        for _, y, dx, _ in own + of_stack:
+            y.zero_(), dx.zero_()
+        h.zero_()
+        torch.cuda.synchronize()
+        with torch.cuda.stream(a):
+            st.step(x0, up, accumulate=False)
+        with torch.cuda.stream(b):
+            for call, *_ in own:
+                call()
+        with torch.cuda.stream(c):
+            st.ctx.rmsnorm(x0, None, T, d, w, 1e-6, None, None, h)
+            for call, *_ in of_stack:
+                call()
+        torch.cuda.synchronize()
+        assert all(torch.equal(getattr(st, n), v) for n, v in zip(names, want)) and torch.equal(h, h0)
+        for (_, y, dx, _), (y0, dx0) in zip(own + of_stack, results):
+            assert torch.equal(y, y0) and torch.equal(dx, dx0)
+    st.ctx.check_status()
+    st.close()
